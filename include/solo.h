@@ -389,6 +389,83 @@ int solo_multi_step_static(int32_t num_tensors, void* const* param_dev, const vo
 int solo_static_status(int* status_out, void* stream);
 
 /*
+ * Gradients before the step.  Between the backward pass and solo_multi_step stand the accumulation
+ * of micro-batches, the global norm and its clipping; the calls below do them over the same kind of
+ * ragged tensor list that the step takes.  (The paper has no counterpart.)  A typical step:
+ *
+ *   solo_grad_accumulate(acc, micro, 1/k, first, ...)    once per micro-batch, k of them
+ *   solo_grad_accumulate_rows(embedding's accumulator, tokens, ...)
+ *   solo_grad_clip_norm(acc -> bf16 gradients, max_norm) or, over several workers,
+ *     solo_grad_norm on each worker's shard, an all-gather of one float, solo_grad_clip
+ *   solo_multi_step on the bf16 gradients
+ *
+ * Sums are taken in binary32 over at most 32 elements of a thread and in binary64 from there on, in
+ * an order that depends on the tensor sizes and the device only: the same inputs give the same bits.
+ * Squares that binary32 cannot hold (overflow, underflow) are summed in binary64.
+ */
+enum { SOLO_DT_F32 = 0, SOLO_DT_BF16 = 1, SOLO_DT_F16 = 2 };       /* element types of a gradient list */
+enum { SOLO_NORM_MAX = 0, SOLO_NORM_1 = 1, SOLO_NORM_2 = 2 };      /* max |g|, sum |g|, sqrt(sum g^2) */
+
+/* Sizes of a tensor list, on the host and on the current device.  Never written after it is made, so
+ * any number of calls, streams and captured graphs may use it at once; it has to outlive them. */
+typedef struct solo_grads solo_grads_t;
+
+/* `numel_host` is a HOST array; 0 is allowed (an empty tensor), and so are lists with no element at all.  Synchronous
+ * (cudaMalloc, cudaMemcpy). */
+int solo_grads_create(const int64_t* numel_host, int num_tensors, solo_grads_t** out);
+/* Synchronizes the device and frees the sizes.  NULL is accepted. */
+int solo_grads_destroy(solo_grads_t* grads);
+/* Bytes of the workspace that the calls with a norm need (16-byte aligned device memory).  Its contents
+ * do not matter before a call nor last after it; calls that may run at the same time need one each. */
+int solo_grads_workspace(const solo_grads_t* grads, size_t* bytes);
+
+/*
+ * A list of gradient tensors.  The struct is host memory; `data` is a DEVICE array with a device
+ * pointer for each tensor (aligned to its elements; 16-byte aligned tensors run faster), which a
+ * call reads when it runs.  Tensors of two lists of a call do not overlap, but for the same list given twice.
+ */
+typedef struct {
+    const solo_grads_t* grads;
+    void* const* data;
+    int32_t dtype;               /* SOLO_DT_* */
+} solo_grad_list_t;
+
+/*
+ * N = |scale| * ||g|| over all tensors, to *norm_dev (device, binary32).  `tensor_norm_dev`: NULL, or a
+ * device array of num_tensors floats for |scale| times every tensor's own norm (0 for an empty one).
+ * NaN and infinities come through.  Asynchronous on `stream`, as all of these calls are.
+ */
+int solo_grad_norm(const solo_grad_list_t* list, int norm_type, float scale, float* norm_dev,
+                   float* tensor_norm_dev, void* workspace_dev, void* stream);
+
+/*
+ * dst = round(src * f), f = scale * min(1, max_norm / (N + 1e-6)), rounded to nearest even.  N is put
+ * together from `norms_dev`, a device array of `num_norms` floats, as the norm of the whole of which
+ * these are the norms of the parts (the workers' shards; one value where there are none); they are
+ * norms of the scaled gradients, as solo_grad_norm gives them.  num_norms = 0: f = scale, a plain
+ * scaling or conversion.  `dst` may be `src` (in place; nothing is read or written then if f is 1) or
+ * a list of the same sizes and any type.  A norm that is NaN makes everything NaN, an infinite one
+ * finite gradients 0; max_norm is finite and not negative.
+ */
+int solo_grad_clip(const solo_grad_list_t* src, const solo_grad_list_t* dst, const float* norms_dev,
+                   int num_norms, int norm_type, float max_norm, float scale, void* stream);
+
+/* solo_grad_norm and solo_grad_clip by its result, in one call. */
+int solo_grad_clip_norm(const solo_grad_list_t* src, const solo_grad_list_t* dst, int norm_type,
+                        float max_norm, float scale, float* norm_dev, float* tensor_norm_dev,
+                        void* workspace_dev, void* stream);
+
+/*
+ * acc = acc + scale * g, or scale * g with `first` (acc is not read then), one rounding for each
+ * element; `acc` is a list of binary32 tensors of the same sizes.  norm_type -1: nothing else
+ * (norm_dev, tensor_norm_dev and workspace_dev are not used); otherwise also the norm of the new acc, from
+ * the same pass.
+ */
+int solo_grad_accumulate(const solo_grad_list_t* acc, const solo_grad_list_t* grad, float scale, int first,
+                         int norm_type, float* norm_dev, float* tensor_norm_dev, void* workspace_dev,
+                         void* stream);
+
+/*
  * Test hook for the bounded wait of the kernels that stage their inputs with asynchronous
  * copies.  The next step launched by this process announces 16 bytes more than it copies for
  * the inputs of tile number `tile` (tiles of 2048 elements, counted over the tensor list), so the

@@ -7,6 +7,7 @@ there, loading raises: there is no other implementation to fall back to.
 from __future__ import annotations
 
 import ctypes as C
+import math
 from pathlib import Path
 
 import torch
@@ -65,6 +66,12 @@ class RawState(C.Structure):
         ("scale_v", C.c_void_p), ("alpha", C.c_void_p),
         ("bits_m", C.c_int32), ("bits_v", C.c_int32), ("block", C.c_int32),
     ]
+
+
+class GradList(C.Structure):
+    """solo_grad_list_t"""
+
+    _fields_ = [("grads", C.c_void_p), ("data", C.c_void_p), ("dtype", C.c_int32)]
 
 
 def hyper(lr=1e-3, beta1=0.8, beta2=0.999, eps=1e-8, weight_decay=0.01, p_quantile=0.1,
@@ -127,12 +134,22 @@ def lib() -> C.CDLL:
     L.solo_launch_count.argtypes = []
     L.solo_launch_count.restype = C.c_int64
     L.solo_strerror.argtypes = [i32]
+    gl, f32 = C.POINTER(GradList), C.c_float
+    L.solo_grads_create.argtypes = [C.POINTER(C.c_int64), i32, C.POINTER(vp)]
+    L.solo_grads_destroy.argtypes = [vp]
+    L.solo_grads_workspace.argtypes = [vp, C.POINTER(C.c_size_t)]
+    L.solo_grad_norm.argtypes = [gl, i32, f32, vp, vp, vp, vp]
+    L.solo_grad_clip.argtypes = [gl, gl, vp, i32, i32, f32, f32, vp]
+    L.solo_grad_clip_norm.argtypes = [gl, gl, i32, f32, f32, vp, vp, vp, vp]
+    L.solo_grad_accumulate.argtypes = [gl, gl, f32, i32, i32, vp, vp, vp, vp]
     L.solo_strerror.restype = C.c_char_p
     for name in ("solo_state_create", "solo_state_create_multi", "solo_state_destroy",
                  "solo_state_bytes", "solo_step", "solo_multi_step", "solo_dequant",
                  "solo_state_raw", "solo_state_info", "solo_state_status", "solo_codebook_m",
                  "solo_set_kernel_policy", "solo_debug_check_fast_log", "solo_state_export_bytes",
-                 "solo_state_export", "solo_state_import"):
+                 "solo_state_export", "solo_state_import", "solo_grads_create", "solo_grads_destroy",
+                 "solo_grads_workspace", "solo_grad_norm", "solo_grad_clip", "solo_grad_clip_norm",
+                 "solo_grad_accumulate"):
         getattr(L, name).restype = C.c_int
     _lib = L
     return L
@@ -388,6 +405,123 @@ def solo_multi_step_host(params: list[torch.Tensor], grads_host: list[torch.Tens
                    C.cast(po, C.c_void_p) if po is not None else None, C.cast(numel, C.c_void_p),
                    int(chunk_elems), state.handle)
     _check(lib().solo_multi_step_host(C.byref(lst), C.byref(h), step, _stream()), "solo_multi_step_host")
+
+
+_GRAD_DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_NORM_TYPE = {math.inf: 0, 1: 1, 2: 2}
+
+
+class GradSet:
+    """Descriptor of a list of gradient tensors of one type: fp32, bf16 or fp16 (built once, reused every step)."""
+
+    def __init__(self, grads: list[torch.Tensor]):
+        if not grads:
+            raise ValueError("a gradient list has at least one tensor")
+        dtype, dev = grads[0].dtype, grads[0].device
+        if dtype not in _GRAD_DTYPE:
+            raise ValueError("gradients must be fp32, bf16 or fp16")
+        for g in grads:
+            if not (g.is_cuda and g.is_contiguous()) or g.dtype != dtype or g.device != dev:
+                raise ValueError("gradients must be contiguous CUDA tensors of one type on one device")
+        if dev.index != torch.cuda.current_device():
+            raise ValueError("gradients must be on the current device")
+        self.grads, self.dtype, self.device = list(grads), dtype, dev
+        self.sizes = [g.numel() for g in grads]
+        self.ptrs = torch.tensor([g.data_ptr() for g in grads], dtype=torch.int64, device=dev)
+        self.handle = C.c_void_p()
+        arr = (C.c_int64 * len(grads))(*self.sizes)
+        _check(lib().solo_grads_create(arr, len(grads), C.byref(self.handle)), "solo_grads_create")
+        n = C.c_size_t()
+        _check(lib().solo_grads_workspace(self.handle, C.byref(n)), "solo_grads_workspace")
+        self.workspace_floats = -(-n.value // 16) * 4
+        self.desc = GradList(self.handle.value, self.ptrs.data_ptr(), _GRAD_DTYPE[dtype])
+
+    def __del__(self):
+        try:
+            if self.handle:
+                lib().solo_grads_destroy(self.handle)
+        except Exception:
+            pass
+
+    def _buffer(self, per_tensor: bool) -> torch.Tensor:
+        """A call's workspace, with room for its results after it: from torch's allocator, so that calls on other streams
+        and captured graphs have their own."""
+        return torch.empty(self.workspace_floats + 1 + (len(self.sizes) if per_tensor else 0), dtype=torch.float32, device=self.device)
+
+
+def _norm_type(p) -> int:
+    if p not in _NORM_TYPE:
+        raise ValueError("norm_type must be 1, 2 or infinity")
+    return _NORM_TYPE[p]
+
+
+def _norm_results(ws: torch.Tensor, gs: GradSet, per_tensor: bool):
+    total = ws[gs.workspace_floats:gs.workspace_floats + 1]
+    return (total, ws[gs.workspace_floats + 1:]) if per_tensor else total
+
+
+def _norm_pointers(ws: torch.Tensor, gs: GradSet, per_tensor: bool) -> tuple:
+    base = ws.data_ptr()
+    norm = base + 4 * gs.workspace_floats
+    return norm, norm + 4 if per_tensor else None, base
+
+
+def solo_grad_norm(gs: GradSet, norm_type=2, scale: float = 1.0, per_tensor: bool = False):
+    """|scale| times the norm (1, 2 or infinity) of the whole list, as a float32 CUDA tensor of one element; with
+    `per_tensor` also one of every tensor's norm.  On the current stream, without waiting, as all of these calls."""
+    ws = gs._buffer(per_tensor)
+    norm, tensors, base = _norm_pointers(ws, gs, per_tensor)
+    rc = (_lib or lib()).solo_grad_norm(C.byref(gs.desc), _norm_type(norm_type), scale, norm, tensors, base, _stream())
+    if rc:
+        _check(rc, "solo_grad_norm")
+    return _norm_results(ws, gs, per_tensor)
+
+
+def solo_grad_clip(src: GradSet, norms, max_norm: float, dst: GradSet = None, norm_type=2, scale: float = 1.0) -> None:
+    """dst (default: src, in place) = src * scale * min(1, max_norm / (N + 1e-6)), N the norm of the whole from the
+    `norms` of its parts (a float32 CUDA tensor); norms=None: scaling and conversion alone."""
+    n = 0
+    if norms is not None:
+        if not norms.is_cuda or norms.dtype != torch.float32 or not norms.is_contiguous() or norms.device != src.device:
+            raise ValueError("norms must be a contiguous float32 tensor on the gradients' device")
+        n = norms.numel()
+        if n == 0:
+            raise ValueError("norms has no element")
+    rc = (_lib or lib()).solo_grad_clip(C.byref(src.desc), C.byref((dst or src).desc), norms.data_ptr() if n else None, n,
+                                        _norm_type(norm_type), max_norm if n else 0.0, scale, _stream())
+    if rc:
+        _check(rc, "solo_grad_clip")
+
+
+def solo_grad_clip_norm(src: GradSet, max_norm: float, dst: GradSet = None, norm_type=2, scale: float = 1.0,
+                        per_tensor: bool = False):
+    """solo_grad_norm, and solo_grad_clip by its result, in one call; returns what solo_grad_norm does."""
+    ws = src._buffer(per_tensor)
+    norm, tensors, base = _norm_pointers(ws, src, per_tensor)
+    rc = (_lib or lib()).solo_grad_clip_norm(C.byref(src.desc), C.byref((dst or src).desc), _norm_type(norm_type), max_norm,
+                                             scale, norm, tensors, base, _stream())
+    if rc:
+        _check(rc, "solo_grad_clip_norm")
+    return _norm_results(ws, src, per_tensor)
+
+
+def solo_grad_accumulate(acc: GradSet, grads: GradSet, scale: float = 1.0, first: bool = False, norm_type=None,
+                         per_tensor: bool = False):
+    """acc (fp32) += scale * grads, or = scale * grads with `first`; with a `norm_type` returns the norm of the new acc
+    as solo_grad_norm does, from the same pass."""
+    if norm_type is None:
+        rc = (_lib or lib()).solo_grad_accumulate(C.byref(acc.desc), C.byref(grads.desc), scale, 1 if first else 0, -1, None, None,
+                                                  None, _stream())
+        if rc:
+            _check(rc, "solo_grad_accumulate")
+        return None
+    ws = acc._buffer(per_tensor)
+    norm, tensors, base = _norm_pointers(ws, acc, per_tensor)
+    rc = (_lib or lib()).solo_grad_accumulate(C.byref(acc.desc), C.byref(grads.desc), scale, 1 if first else 0,
+                                              _norm_type(norm_type), norm, tensors, base, _stream())
+    if rc:
+        _check(rc, "solo_grad_accumulate")
+    return _norm_results(ws, acc, per_tensor)
 
 
 def codebook_m(bits: int) -> torch.Tensor:

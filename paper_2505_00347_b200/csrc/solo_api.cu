@@ -13,6 +13,7 @@
 
 #include "solo_device.cuh"
 #include "solo_dispatch.h"
+#include "solo_host.h"
 
 using solo::StepArgs;
 
@@ -142,7 +143,9 @@ __global__ void fill_f32(float* p, int64_t n, float v) {
         p[i] = v;
 }
 
-int sm_count(int device) {
+}  // namespace
+
+int solo::sm_count(int device) {
     static std::mutex mu;
     static int cached[64];
     static bool have[64];
@@ -157,6 +160,12 @@ int sm_count(int device) {
     }
     return cached[device];
 }
+
+void solo::count_launch() { g_launches.fetch_add(1, std::memory_order_relaxed); }
+
+namespace {
+
+using solo::sm_count;
 
 int check_hyper(const solo_hyper_t* h, int64_t step) {
     if (!h || step < 1) return SOLO_EINVAL;

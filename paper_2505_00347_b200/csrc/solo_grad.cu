@@ -1,0 +1,664 @@
+// Gradient lists before the step: global norm, clipping, accumulation over micro-batches (include/solo.h).
+//
+// All of these are streams over ragged lists of tensors, a read of 2 or 4 bytes per element and up to
+// 8 bytes written and read besides, and one or two operations on it: bound by HBM.  One kernel template serves them.  The list
+// is cut into tiles of 8192 elements of one tensor each, a CTA takes a contiguous share of the tiles, so that its search
+// for a tensor happens once and its sums need one partial per tensor that it touches.
+//
+// Sums.  A thread sums the (at most 32) powers that it takes from a tile in binary32 and adds that to a binary64 sum;
+// threads, CTAs and tensors are summed in binary64 in a fixed order (no atomics), so results do not vary from call to call.
+// A binary32 sum that overflowed, or is so small that squares may have been lost below 2^-149, is taken again in binary64
+// from the values still in registers.  Maxima are maxima of magnitude bit patterns, above all of which NaN lies.
+#include "solo.h"
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <map>
+#include <mutex>
+#include <new>
+#include <vector>
+
+#include "solo_device.cuh"
+#include "solo_host.h"
+
+namespace solo {
+namespace {
+
+constexpr int GCTA = 256;                  // threads per CTA
+constexpr int GV = 8;                      // elements per thread and vector: 16 bytes of bf16, 32 of fp32
+constexpr int GU = 4;                      // vectors per thread and tile
+constexpr int GTILE = GCTA * GV * GU;      // elements per tile
+constexpr int GCTAS_PER_SM = 8;            // most CTAs per SM that a launch takes (bounds the workspace)
+
+enum { OP_NORM = 0, OP_CLIP = 1, OP_ACC = 2, OP_ACC_FIRST = 3 };
+
+struct GradArgs {
+    const void* const* src;      // gradients read
+    void* const* dst;            // what is written: clipped gradients, accumulators
+    const int64_t* numel;
+    const int64_t* tile_start;   // [T + 1]
+    int64_t tiles;
+    int32_t num_tensors;
+    int32_t norm_type;           // of the factor's norm (OP_CLIP)
+    int32_t num_partials, num_norms;
+    float scale, max_norm;
+    double* cta_sum;             // [grid] what a CTA's share of the list sums to; null: no norm
+    double* slots;               // [grid + T] partial of tensor t from CTA c at c + t: a CTA's last tensor is the next one's
+                                 // first at the earliest, so no two partials share an index; null: no per-tensor norms
+    const double* partials;      // OP_CLIP: cta_sum of the kernel before, or
+    const float* norms;          // norms of the parts
+    float* norm_out;             // null, or where the norm goes
+};
+
+// ---- element types ------------------------------------------------------------------------------------------------
+
+template <int DT> constexpr int DT_BYTES = DT == SOLO_DT_F32 ? 4 : 2;
+
+__device__ __forceinline__ float elem_load(const void* p, int64_t i, std::integral_constant<int, SOLO_DT_F32>) { return ((const float*)p)[i]; }
+__device__ __forceinline__ float elem_load(const void* p, int64_t i, std::integral_constant<int, SOLO_DT_BF16>) {
+    return __uint_as_float((uint32_t)((const uint16_t*)p)[i] << 16);
+}
+__device__ __forceinline__ float elem_load(const void* p, int64_t i, std::integral_constant<int, SOLO_DT_F16>) {
+    return __half2float(((const __half*)p)[i]);
+}
+__device__ __forceinline__ void elem_store(void* p, int64_t i, float v, std::integral_constant<int, SOLO_DT_F32>) { ((float*)p)[i] = v; }
+__device__ __forceinline__ void elem_store(void* p, int64_t i, float v, std::integral_constant<int, SOLO_DT_BF16>) {
+    ((__nv_bfloat16*)p)[i] = __float2bfloat16_rn(v);
+}
+__device__ __forceinline__ void elem_store(void* p, int64_t i, float v, std::integral_constant<int, SOLO_DT_F16>) {
+    ((__half*)p)[i] = __float2half_rn(v);
+}
+
+// Eight consecutive elements as they lie in memory.
+template <int DT> struct Raw8 { uint4 q[DT_BYTES<DT> / 2]; };
+
+template <int DT> __device__ __forceinline__ Raw8<DT> load8(const void* p, int64_t i) {
+    const uint4* a = reinterpret_cast<const uint4*>((const char*)p + i * DT_BYTES<DT>);
+    Raw8<DT> r;
+#pragma unroll
+    for (int k = 0; k < DT_BYTES<DT> / 2; ++k) r.q[k] = a[k];
+    return r;
+}
+
+template <int DT> __device__ __forceinline__ void unpack8(const Raw8<DT>& r, float (&v)[8]) {
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(&r);
+    if constexpr (DT == SOLO_DT_F32) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(w[k]);
+    } else if constexpr (DT == SOLO_DT_BF16) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            v[2 * k] = __uint_as_float(w[k] << 16);
+            v[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[k]));
+            v[2 * k] = f.x;
+            v[2 * k + 1] = f.y;
+        }
+    }
+}
+
+template <int DT> __device__ __forceinline__ void store8(void* p, int64_t i, const float (&v)[8]) {
+    uint4* a = reinterpret_cast<uint4*>((char*)p + i * DT_BYTES<DT>);
+    Raw8<DT> r;
+    uint32_t* w = reinterpret_cast<uint32_t*>(&r);
+    if constexpr (DT == SOLO_DT_F32) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = __float_as_uint(v[k]);
+    } else if constexpr (DT == SOLO_DT_BF16) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
+            w[k] = *reinterpret_cast<const uint32_t*>(&b);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const __half2 b = __floats2half2_rn(v[2 * k], v[2 * k + 1]);
+            w[k] = *reinterpret_cast<const uint32_t*>(&b);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < DT_BYTES<DT> / 2; ++k) a[k] = r.q[k];
+}
+
+// ---- sums ---------------------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ double max_nan(double a, double b) { return (b > a || b != b) ? b : a; }
+template <int NT> __device__ __forceinline__ double join(double a, double b) { return NT == SOLO_NORM_MAX ? max_nan(a, b) : a + b; }
+__device__ __forceinline__ double join(int nt, double a, double b) { return nt == SOLO_NORM_MAX ? max_nan(a, b) : a + b; }
+
+// A thread's sum of powers (p = 1, 2: binary64) or its largest magnitude (as a bit pattern).
+template <int NT> struct Sum {
+    double s = 0.0;
+    uint32_t m = 0;
+    template <int N> __device__ __forceinline__ void add(const float (&v)[N]) {
+        if constexpr (NT == SOLO_NORM_MAX) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) m = max(m, __float_as_uint(v[k]) & 0x7FFFFFFFu);
+        } else if constexpr (NT == SOLO_NORM_1) {
+            float c[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int k = 0; k < N; ++k) c[k & 1] = c[k & 1] + fabsf(v[k]);
+            const float f = c[0] + c[1];
+            if (f < __int_as_float(0x7F800000)) {
+                s += (double)f;
+            } else {
+#pragma unroll
+                for (int k = 0; k < N; ++k) s += (double)fabsf(v[k]);
+            }
+        } else if constexpr (NT == SOLO_NORM_2) {
+            float c[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int k = 0; k < N; ++k) c[k & 1] = __fmaf_rn(v[k], v[k], c[k & 1]);
+            const float f = c[0] + c[1];
+            // Above 2^-100, what N <= 32 squares lost below 2^-149 is less than 2^-44 of the sum.
+            if (f >= 0x1p-100f && f < __int_as_float(0x7F800000)) {
+                s += (double)f;
+            } else {
+                uint32_t any = 0;
+#pragma unroll
+                for (int k = 0; k < N; ++k) any |= __float_as_uint(v[k]);
+                if (any & 0x7FFFFFFFu) {
+#pragma unroll
+                    for (int k = 0; k < N; ++k) s = __fma_rn((double)v[k], (double)v[k], s);
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ double value() const { return NT == SOLO_NORM_MAX ? (double)__uint_as_float(m) : s; }
+    __device__ __forceinline__ void clear() { s = 0.0; m = 0; }
+};
+
+// Sum over the CTA, in every thread.  `box`: one double per warp, free again after the next barrier but one.
+__device__ __forceinline__ double cta_join(int nt, double v, double* box) {
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) v = join(nt, v, __shfl_xor_sync(0xFFFFFFFFu, v, d));
+    if ((threadIdx.x & 31) == 0) box[threadIdx.x >> 5] = v;
+    __syncthreads();
+    double r = box[0];
+#pragma unroll
+    for (int w = 1; w < GCTA / 32; ++w) r = join(nt, r, box[w]);
+    return r;
+}
+
+__device__ __forceinline__ double root(int nt, double s) { return nt == SOLO_NORM_2 ? sqrt(s) : s; }
+
+// N of a clip (every CTA computes it for itself, in the same order: a few partials per thread, from L2), and its factor.
+__device__ __forceinline__ float clip_factor(const GradArgs& a, double* box, double* norm) {
+    double s = 0.0;
+    for (int i = threadIdx.x; i < a.num_partials; i += GCTA) s = join(a.norm_type, s, a.partials[i]);
+    for (int i = threadIdx.x; i < a.num_norms; i += GCTA) {
+        const double v = fabs((double)a.norms[i]);
+        s = join(a.norm_type, s, a.norm_type == SOLO_NORM_2 ? v * v : v);
+    }
+    s = root(a.norm_type, cta_join(a.norm_type, s, box));
+    if (a.num_partials) s *= fabs((double)a.scale);
+    *norm = s;
+    double c = 1.0;
+    if (a.num_partials + a.num_norms) {
+        c = (double)a.max_norm / (s + 1e-6);
+        if (c > 1.0) c = 1.0;                    // a NaN stays
+    }
+    return (float)((double)a.scale * c);
+}
+
+// Largest t with tile_start[t] <= x: 32 places at a time, the whole warp together.
+__device__ __forceinline__ int find_tensor(const int64_t* tile_start, int num_tensors, int64_t x) {
+    int lo = 0, hi = num_tensors;
+    const int lane = threadIdx.x & 31;
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 31) / 32;
+        const int probe = lo + (lane + 1) * step;
+        const bool below = probe < hi && tile_start[probe] <= x;
+        const int n = __popc(__ballot_sync(0xFFFFFFFFu, below));     // starts do not decrease: the lanes below are the first ones
+        lo += n * step;
+        hi = min(hi, lo + step);
+    }
+    return lo;
+}
+
+// ---- the kernel -----------------------------------------------------------------------------------------------------
+
+// DS: type read (gradients); DD: type written; NT: norm type or -1.
+template <int OP, int DS, int DD, int NT> __global__ __launch_bounds__(GCTA) void grad_kernel(const __grid_constant__ GradArgs a) {
+    using S = std::integral_constant<int, DS>;
+    using D = std::integral_constant<int, DD>;
+    constexpr bool WRITES = OP != OP_NORM;
+    constexpr bool SUMS = NT >= 0;
+    __shared__ double box[2][GCTA / 32];
+    int turn = 0;
+    pdl_wait();
+    pdl_release();
+    const int64_t grid = gridDim.x, c = blockIdx.x;
+    const int64_t lo = a.tiles * c / grid, hi = a.tiles * (c + 1) / grid;
+    float f = a.scale;
+    if constexpr (OP == OP_CLIP) {
+        double norm;
+        f = clip_factor(a, box[turn], &norm);
+        turn ^= 1;
+        if (a.norm_out && c == 0 && threadIdx.x == 0) *a.norm_out = (float)norm;
+    }
+    Sum<NT> sum;
+    double share = 0.0;
+    int t = lo < hi ? find_tensor(a.tile_start, a.num_tensors, lo) : 0;
+    for (int64_t x = lo; x < hi;) {
+        while (a.tile_start[t + 1] <= x) ++t;                       // past empty tensors
+        const int64_t t0 = a.tile_start[t];
+        const int64_t xe = min(hi, a.tile_start[t + 1]);
+        const int64_t n = a.numel[t];
+        const void* const s = a.src[t];
+        void* const d = WRITES ? a.dst[t] : nullptr;
+        // Elements before the first place where vectors of both sides start on a 16-byte boundary; none: element by element.
+        int head = 0;
+        bool vec;
+        {
+            const uintptr_t sa = (uintptr_t)s, da = (uintptr_t)d;
+            constexpr int narrow = WRITES && DT_BYTES<DD> < DT_BYTES<DS>;
+            if (narrow) head = (int)((16 - (da & 15)) & 15) / DT_BYTES<DD>;
+            else head = (int)((16 - (sa & 15)) & 15) / DT_BYTES<DS>;
+            vec = ((sa + head * DT_BYTES<DS>) & 15) == 0 && (!WRITES || ((da + head * DT_BYTES<DD>) & 15) == 0);
+            if (!vec) head = 0;
+        }
+        if (OP == OP_CLIP && DS == DD && f == 1.0f && s == d) x = xe;       // in place, by one: nothing changes
+        for (; x < xe; ++x) {
+            const int64_t base = head + (x - t0) * GTILE;
+            int64_t e0 = x == t0 ? 0 : base, e1 = min(n, base + GTILE);
+            if (vec && base + GTILE <= n) {
+                Raw8<DS> g[GU];
+                [[maybe_unused]] Raw8<SOLO_DT_F32> acc[OP == OP_ACC ? GU : 1];
+#pragma unroll
+                for (int u = 0; u < GU; ++u) {
+                    const int64_t i = base + (u * GCTA + (int)threadIdx.x) * GV;
+                    g[u] = load8<DS>(s, i);
+                    if constexpr (OP == OP_ACC) acc[u] = load8<SOLO_DT_F32>(d, i);
+                }
+                float v[GU * GV];
+#pragma unroll
+                for (int u = 0; u < GU; ++u) {
+                    float w[GV];
+                    unpack8<DS>(g[u], w);
+                    if constexpr (OP == OP_ACC) {
+                        float b[GV];
+                        unpack8<SOLO_DT_F32>(acc[u], b);
+#pragma unroll
+                        for (int k = 0; k < GV; ++k) w[k] = __fmaf_rn(f, w[k], b[k]);
+                    } else if constexpr (WRITES) {
+#pragma unroll
+                        for (int k = 0; k < GV; ++k) w[k] = f * w[k];
+                    }
+                    if constexpr (WRITES) store8<DD>(d, base + (u * GCTA + (int)threadIdx.x) * GV, w);
+#pragma unroll
+                    for (int k = 0; k < GV; ++k) v[u * GV + k] = w[k];
+                }
+                if constexpr (SUMS) sum.add(v);
+                e1 = base;                                          // what is left: the elements before the first vector
+            }
+            for (int64_t i0 = e0; i0 < e1; i0 += GCTA * 8) {
+                float w[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const int64_t i = i0 + k * GCTA + threadIdx.x;
+                    w[k] = i < e1 ? elem_load(s, i, S{}) : 0.0f;
+                    if constexpr (OP == OP_ACC) w[k] = i < e1 ? __fmaf_rn(f, w[k], elem_load(d, i, D{})) : 0.0f;
+                    else if constexpr (WRITES) w[k] = f * w[k];
+                }
+                if constexpr (WRITES) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const int64_t i = i0 + k * GCTA + threadIdx.x;
+                        if (i < e1) elem_store(d, i, w[k], D{});
+                    }
+                }
+                if constexpr (SUMS) sum.add(w);
+            }
+        }
+        if constexpr (SUMS) {
+            if (a.slots) {
+                const double r = cta_join(NT, sum.value(), box[turn]);
+                turn ^= 1;
+                if (threadIdx.x == 0) a.slots[c + t] = r;
+                share = join<NT>(share, r);
+                sum.clear();
+            }
+        }
+    }
+    if constexpr (SUMS) {
+        if (!a.slots) share = cta_join(NT, sum.value(), box[turn]);
+        if (threadIdx.x == 0) a.cta_sum[c] = share;
+    }
+}
+
+// Norms from the partials: the total in CTA 0 (where norm_out is given), a tensor per warp in the others.
+struct FinishArgs {
+    const double* cta_sum;
+    const double* slots;
+    const int64_t* tile_start;
+    int64_t tiles;
+    int32_t grid, num_tensors, norm_type;
+    float scale;
+    float* norm_out;
+    float* tensor_norm;
+};
+
+__global__ __launch_bounds__(GCTA) void grad_finish_kernel(const __grid_constant__ FinishArgs a) {
+    __shared__ double box[GCTA / 32];
+    pdl_wait();
+    pdl_release();
+    const double scale = fabs((double)a.scale);
+    if (blockIdx.x == 0) {
+        if (!a.norm_out) return;
+        double s = 0.0;
+        for (int i = threadIdx.x; i < a.grid; i += GCTA) s = join(a.norm_type, s, a.cta_sum[i]);
+        s = cta_join(a.norm_type, s, box);
+        if (threadIdx.x == 0) *a.norm_out = (float)(scale * root(a.norm_type, s));
+        return;
+    }
+    const int t = (blockIdx.x - 1) * (GCTA / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (t >= a.num_tensors) return;
+    const int64_t t0 = a.tile_start[t], t1 = a.tile_start[t + 1];
+    double s = 0.0;
+    if (t0 < t1) {
+        // tile x lies in the share of CTA ((x + 1) grid - 1) / tiles
+        const int64_t c0 = ((t0 + 1) * a.grid - 1) / a.tiles, c1 = (t1 * a.grid - 1) / a.tiles;
+        for (int64_t c = c0 + lane; c <= c1; c += 32) s = join(a.norm_type, s, a.slots[c + t]);
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) s = join(a.norm_type, s, __shfl_xor_sync(0xFFFFFFFFu, s, d));
+    if (lane == 0) a.tensor_norm[t] = (float)(scale * root(a.norm_type, s));
+}
+
+// ---- instances --------------------------------------------------------------------------------------------------------
+
+using GradKernel = void (*)(const GradArgs);
+
+template <int OP, int DS, int DD> GradKernel by_norm(int nt) {
+    if constexpr (OP == OP_CLIP) return grad_kernel<OP, DS, DD, -1>;
+    else switch (nt) {
+        case SOLO_NORM_MAX: return grad_kernel<OP, DS, DD, SOLO_NORM_MAX>;
+        case SOLO_NORM_1: return grad_kernel<OP, DS, DD, SOLO_NORM_1>;
+        case SOLO_NORM_2: return grad_kernel<OP, DS, DD, SOLO_NORM_2>;
+        default:
+            if constexpr (OP == OP_NORM) return nullptr;
+            else return grad_kernel<OP, DS, DD, -1>;
+    }
+}
+template <int OP, int DS> GradKernel by_dst(int dd, int nt) {
+    if constexpr (OP != OP_CLIP) return by_norm<OP, DS, SOLO_DT_F32>(nt);
+    else switch (dd) {
+        case SOLO_DT_F32: return by_norm<OP, DS, SOLO_DT_F32>(nt);
+        case SOLO_DT_BF16: return by_norm<OP, DS, SOLO_DT_BF16>(nt);
+        default: return by_norm<OP, DS, SOLO_DT_F16>(nt);
+    }
+}
+template <int OP> GradKernel by_src(int ds, int dd, int nt) {
+    switch (ds) {
+        case SOLO_DT_F32: return by_dst<OP, SOLO_DT_F32>(dd, nt);
+        case SOLO_DT_BF16: return by_dst<OP, SOLO_DT_BF16>(dd, nt);
+        default: return by_dst<OP, SOLO_DT_F16>(dd, nt);
+    }
+}
+GradKernel grad_kernel_for(int op, int ds, int dd, int nt) {
+    switch (op) {
+        case OP_NORM: return by_src<OP_NORM>(ds, dd, nt);
+        case OP_CLIP: return by_src<OP_CLIP>(ds, dd, nt);
+        case OP_ACC: return by_src<OP_ACC>(ds, dd, nt);
+        default: return by_src<OP_ACC_FIRST>(ds, dd, nt);
+    }
+}
+
+// Resident CTAs per SM, at most GCTAS_PER_SM; 0 on error.
+int grad_occupancy(GradKernel k, int device) {
+    static std::mutex mu;
+    static std::map<std::pair<int, const void*>, int> cache;
+    std::lock_guard<std::mutex> lk(mu);
+    const auto key = std::make_pair(device, (const void*)k);
+    const auto it = cache.find(key);
+    if (it != cache.end()) return it->second;
+    int n = 0;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, (const void*)k, GCTA, 0) != cudaSuccess) {
+        cudaGetLastError();
+        return 0;
+    }
+    n = std::min(n, GCTAS_PER_SM);
+    cache[key] = n;
+    return n;
+}
+
+int launch(const void* k, unsigned grid, void** params, cudaStream_t stream) {
+    cudaLaunchAttribute attr = {};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;    // see pdl_wait
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(GCTA);
+    cfg.stream = stream;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelExC(&cfg, k, params) != cudaSuccess) {
+        cudaGetLastError();
+        return SOLO_ECUDA;
+    }
+    count_launch();
+    return SOLO_OK;
+}
+
+}  // namespace
+}  // namespace solo
+
+struct solo_grads {
+    int device = 0;
+    int num_tensors = 0;
+    int64_t tiles = 0;
+    std::vector<int64_t> numel;
+    int64_t* geom = nullptr;      // device: numel[T] | tile_start[T + 1]
+};
+
+namespace {
+
+using namespace solo;
+
+bool valid_dtype(int d) { return d >= SOLO_DT_F32 && d <= SOLO_DT_F16; }
+bool valid_norm(int n) { return n >= SOLO_NORM_MAX && n <= SOLO_NORM_2; }
+
+int check_list(const solo_grad_list_t* l) {
+    if (!l || !l->grads || !l->data || !valid_dtype(l->dtype)) return SOLO_EINVAL;
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return SOLO_ECUDA; }
+    return dev == l->grads->device ? SOLO_OK : SOLO_ESTATE;
+}
+
+int check_pair(const solo_grad_list_t* a, const solo_grad_list_t* b) {
+    int rc = check_list(a);
+    if (rc == SOLO_OK) rc = check_list(b);
+    if (rc != SOLO_OK) return rc;
+    return a->grads == b->grads || a->grads->numel == b->grads->numel ? SOLO_OK : SOLO_ESTATE;
+}
+
+int check_norm(int norm_type, const float* norm_dev, const void* workspace) {
+    if (!valid_norm(norm_type) || !norm_dev || !workspace) return SOLO_EINVAL;
+    return ((uintptr_t)workspace & 15u) ? SOLO_EALIGN : SOLO_OK;
+}
+
+// One pass over the list; *grid_out: CTAs launched (what the partials are of).
+int pass(int op, const solo_grad_list_t* src, const solo_grad_list_t* dst, int norm_type, GradArgs a, cudaStream_t stream,
+         int* grid_out = nullptr) {
+    const solo_grads* g = src->grads;
+    const GradKernel k = grad_kernel_for(op, src->dtype, dst ? dst->dtype : 0, norm_type);
+    if (!k) return SOLO_EINVAL;
+    const int per_sm = grad_occupancy(k, g->device);
+    if (per_sm <= 0) return SOLO_ECUDA;
+    a.src = (const void* const*)src->data;
+    a.dst = dst ? dst->data : nullptr;
+    a.numel = g->geom;
+    a.tile_start = g->geom + g->num_tensors;
+    a.tiles = g->tiles;
+    a.num_tensors = g->num_tensors;
+    const int64_t grid = std::max<int64_t>(1, std::min<int64_t>(g->tiles, (int64_t)sm_count(g->device) * per_sm));
+    if (grid_out) *grid_out = (int)grid;
+    void* params[] = {&a};
+    return launch((const void*)k, (unsigned)grid, params, stream);
+}
+
+int finish(const solo_grads* g, const GradArgs& a, int grid, int norm_type, float scale, float* norm_dev, float* tensor_norm_dev,
+           cudaStream_t stream) {
+    FinishArgs f;
+    std::memset(&f, 0, sizeof(f));
+    f.cta_sum = a.cta_sum;
+    f.slots = a.slots;
+    f.tile_start = g->geom + g->num_tensors;
+    f.tiles = g->tiles;
+    f.grid = grid;
+    f.num_tensors = g->num_tensors;
+    f.norm_type = norm_type;
+    f.scale = scale;
+    f.norm_out = norm_dev;
+    f.tensor_norm = tensor_norm_dev;
+    void* params[] = {&f};
+    const unsigned blocks = 1u + (tensor_norm_dev ? (unsigned)((g->num_tensors + GCTA / 32 - 1) / (GCTA / 32)) : 0u);
+    return launch((const void*)grad_finish_kernel, blocks, params, stream);
+}
+
+size_t most_ctas(const solo_grads* g) { return (size_t)sm_count(g->device) * GCTAS_PER_SM; }
+
+GradArgs norm_args(const solo_grads* g, void* workspace, const float* tensor_norm_dev) {
+    GradArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.cta_sum = (double*)workspace;
+    a.slots = tensor_norm_dev ? (double*)workspace + most_ctas(g) : nullptr;
+    return a;
+}
+
+}  // namespace
+
+extern "C" {
+
+int solo_grads_create(const int64_t* numel_host, int num_tensors, solo_grads_t** out) {
+    if (!out) return SOLO_EINVAL;
+    *out = nullptr;
+    if (!numel_host || num_tensors < 1) return SOLO_EINVAL;
+    for (int t = 0; t < num_tensors; ++t)
+        if (numel_host[t] < 0 || numel_host[t] > ((int64_t)1 << 48)) return SOLO_EINVAL;
+    solo_grads* g = nullptr;
+    try {
+        g = new solo_grads();
+        g->numel.assign(numel_host, numel_host + num_tensors);
+        std::vector<int64_t> geom(g->numel);
+        for (int t = 0; t < num_tensors; ++t) {
+            geom.push_back(g->tiles);
+            g->tiles += (numel_host[t] + GTILE - 1) / GTILE;
+        }
+        geom.push_back(g->tiles);
+        g->num_tensors = num_tensors;
+        if (g->tiles > ((int64_t)1 << 40)) { delete g; return SOLO_EINVAL; }       // share arithmetic: tiles * CTAs in 64 bits
+        if (cudaGetDevice(&g->device) != cudaSuccess) { cudaGetLastError(); delete g; return SOLO_ECUDA; }
+        if (cudaMalloc((void**)&g->geom, geom.size() * 8) != cudaSuccess) { cudaGetLastError(); delete g; return SOLO_ENOMEM; }
+        if (cudaMemcpy(g->geom, geom.data(), geom.size() * 8, cudaMemcpyHostToDevice) != cudaSuccess) {
+            cudaGetLastError();
+            cudaFree(g->geom);
+            delete g;
+            return SOLO_ECUDA;
+        }
+    } catch (const std::bad_alloc&) {
+        if (g) delete g;
+        return SOLO_ENOMEM;
+    }
+    *out = g;
+    return SOLO_OK;
+}
+
+int solo_grads_destroy(solo_grads_t* g) {
+    if (!g) return SOLO_OK;
+    cudaDeviceSynchronize();
+    cudaFree(g->geom);
+    delete g;
+    return SOLO_OK;
+}
+
+int solo_grads_workspace(const solo_grads_t* g, size_t* bytes) {
+    if (!g || !bytes) return SOLO_EINVAL;
+    *bytes = (2 * most_ctas(g) + (size_t)g->num_tensors) * sizeof(double);
+    return SOLO_OK;
+}
+
+int solo_grad_norm(const solo_grad_list_t* list, int norm_type, float scale, float* norm_dev, float* tensor_norm_dev,
+                   void* workspace_dev, void* stream) {
+    int rc = check_list(list);
+    if (rc == SOLO_OK) rc = check_norm(norm_type, norm_dev, workspace_dev);
+    if (rc != SOLO_OK) return rc;
+    if (!std::isfinite(scale)) return SOLO_EINVAL;
+    const GradArgs a = norm_args(list->grads, workspace_dev, tensor_norm_dev);
+    int grid = 0;
+    rc = pass(OP_NORM, list, nullptr, norm_type, a, (cudaStream_t)stream, &grid);
+    if (rc != SOLO_OK) return rc;
+    return finish(list->grads, a, grid, norm_type, scale, norm_dev, tensor_norm_dev, (cudaStream_t)stream);
+}
+
+int solo_grad_clip(const solo_grad_list_t* src, const solo_grad_list_t* dst, const float* norms_dev, int num_norms, int norm_type,
+                   float max_norm, float scale, void* stream) {
+    const int rc = check_pair(src, dst);
+    if (rc != SOLO_OK) return rc;
+    if (num_norms < 0 || (num_norms && !norms_dev) || !valid_norm(norm_type)) return SOLO_EINVAL;
+    if (!std::isfinite(scale) || (num_norms && !(std::isfinite(max_norm) && max_norm >= 0.0f))) return SOLO_EINVAL;
+    GradArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.norms = norms_dev;
+    a.num_norms = num_norms;
+    a.norm_type = norm_type;
+    a.max_norm = max_norm;
+    a.scale = scale;
+    return pass(OP_CLIP, src, dst, -1, a, (cudaStream_t)stream);
+}
+
+int solo_grad_clip_norm(const solo_grad_list_t* src, const solo_grad_list_t* dst, int norm_type, float max_norm, float scale,
+                        float* norm_dev, float* tensor_norm_dev, void* workspace_dev, void* stream) {
+    int rc = check_pair(src, dst);
+    if (rc == SOLO_OK) rc = check_norm(norm_type, norm_dev, workspace_dev);
+    if (rc != SOLO_OK) return rc;
+    if (!std::isfinite(scale) || !std::isfinite(max_norm) || !(max_norm >= 0.0f)) return SOLO_EINVAL;
+    const GradArgs n = norm_args(src->grads, workspace_dev, tensor_norm_dev);
+    int grid = 0;
+    rc = pass(OP_NORM, src, nullptr, norm_type, n, (cudaStream_t)stream, &grid);
+    if (rc != SOLO_OK) return rc;
+    if (tensor_norm_dev) {
+        rc = finish(src->grads, n, grid, norm_type, scale, nullptr, tensor_norm_dev, (cudaStream_t)stream);
+        if (rc != SOLO_OK) return rc;
+    }
+    GradArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.partials = n.cta_sum;
+    a.num_partials = grid;
+    a.norm_type = norm_type;
+    a.max_norm = max_norm;
+    a.scale = scale;
+    a.norm_out = norm_dev;
+    return pass(OP_CLIP, src, dst, -1, a, (cudaStream_t)stream);
+}
+
+int solo_grad_accumulate(const solo_grad_list_t* acc, const solo_grad_list_t* grad, float scale, int first, int norm_type,
+                         float* norm_dev, float* tensor_norm_dev, void* workspace_dev, void* stream) {
+    int rc = check_pair(acc, grad);
+    if (rc != SOLO_OK) return rc;
+    if (acc->dtype != SOLO_DT_F32 || !std::isfinite(scale)) return SOLO_EINVAL;
+    GradArgs a;
+    std::memset(&a, 0, sizeof(a));
+    if (norm_type != -1) {
+        rc = check_norm(norm_type, norm_dev, workspace_dev);
+        if (rc != SOLO_OK) return rc;
+        a = norm_args(acc->grads, workspace_dev, tensor_norm_dev);
+    }
+    a.scale = scale;
+    int grid = 0;
+    rc = pass(first ? OP_ACC_FIRST : OP_ACC, grad, acc, norm_type, a, (cudaStream_t)stream, &grid);
+    if (rc != SOLO_OK || norm_type == -1) return rc;
+    return finish(acc->grads, a, grid, norm_type, 1.0f, norm_dev, tensor_norm_dev, (cudaStream_t)stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,53 @@
+"""Refusals of the gradient-list calls that need no GPU: arguments are looked at before the device is."""
+import ctypes as C
+
+import pytest
+
+
+@pytest.fixture(scope="module")
+def B():
+    import __graft_entry__ as ge
+    ge.build()
+    from paper_2505_00347_b200 import binding
+    return binding
+
+
+def create(B, sizes, n=None):
+    h = C.c_void_p(1)
+    arr = (C.c_int64 * max(1, len(sizes)))(*sizes)
+    return B.lib().solo_grads_create(arr, len(sizes) if n is None else n, C.byref(h)), h
+
+
+def test_sizes_are_checked(B):
+    for sizes, n in (([], None), ([1], -1), ([-1], None), ([5, -3], None), ([(1 << 48) + 1], None)):
+        rc, h = create(B, sizes, n)
+        assert rc == B.SOLO_EINVAL and not h.value, (sizes, n)
+    assert B.lib().solo_grads_create(None, 1, C.byref(C.c_void_p())) == B.SOLO_EINVAL
+    assert B.lib().solo_grads_create((C.c_int64 * 1)(4), 1, None) == B.SOLO_EINVAL
+    assert B.lib().solo_grads_destroy(None) == B.SOLO_OK
+    assert B.lib().solo_grads_workspace(None, C.byref(C.c_size_t())) == B.SOLO_EINVAL
+
+
+def test_lists_without_sizes_data_or_type_are_refused(B):
+    L = B.lib()
+    for bad in (B.GradList(None, 16, 0), B.GradList(None, None, 0)):
+        p = C.byref(bad)
+        assert L.solo_grad_norm(p, 2, 1.0, 16, None, 16, None) == B.SOLO_EINVAL
+        assert L.solo_grad_clip(p, p, 16, 1, 2, 1.0, 1.0, None) == B.SOLO_EINVAL
+        assert L.solo_grad_clip_norm(p, p, 2, 1.0, 1.0, 16, None, 16, None) == B.SOLO_EINVAL
+        assert L.solo_grad_accumulate(p, p, 1.0, 0, -1, None, None, None, None) == B.SOLO_EINVAL
+    assert L.solo_grad_norm(None, 2, 1.0, 16, None, 16, None) == B.SOLO_EINVAL
+
+
+def test_python_checks_come_before_the_library(B):
+    import torch
+    with pytest.raises(ValueError):
+        B.GradSet([])
+    with pytest.raises(ValueError):
+        B.GradSet([torch.zeros(4)])                       # not on a GPU
+    with pytest.raises(ValueError):
+        B.GradSet([torch.zeros(4, dtype=torch.float64)])
+    for p in (0, 3, -1, "2"):
+        with pytest.raises(ValueError):
+            B._norm_type(p)
+    assert (B._norm_type(2.0), B._norm_type(1), B._norm_type(float("inf"))) == (2, 1, 0)
