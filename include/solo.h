@@ -466,6 +466,28 @@ int solo_grad_accumulate(const solo_grad_list_t* acc, const solo_grad_list_t* gr
                          void* stream);
 
 /*
+ * The gradient of an embedding, added to its accumulator: acc[tokens[i], :] += scale * grad[i, :], i = 0 .. num_tokens - 1.
+ * Tokens outside [0, num_rows) (padding, masked positions) contribute nothing, whatever their rows hold; rows of acc that no
+ * token names stay as they are.  The rows of one token are summed in their order, in pieces of fewer than 96 in binary32 and over
+ * the pieces in binary64, for 65,536 tokens at a time, and each such sum is added with one rounding: the same inputs
+ * give the same bits.
+ */
+typedef struct {
+    float* acc;                  /* device [num_rows, width], binary32 */
+    int64_t num_rows;            /* 1 .. 2^31 - 1 */
+    int64_t width;               /* 1 .. 2^24 */
+    const void* tokens;          /* device [num_tokens] */
+    int32_t token_bytes;         /* 4: int32, 8: int64 */
+    int32_t grad_dtype;          /* SOLO_DT_* */
+    const void* grad;            /* device: row i starts grad_stride * i elements after row 0; does not overlap acc */
+    int64_t grad_stride;         /* >= 0 */
+    int64_t num_tokens;          /* 0 .. 2^40 */
+} solo_grad_rows_t;
+/* `workspace_dev`: 16-byte aligned device memory of solo_grad_rows_workspace's size, as for solo_grads_workspace. */
+int solo_grad_rows_workspace(int64_t num_tokens, int64_t width, size_t* bytes);
+int solo_grad_accumulate_rows(const solo_grad_rows_t* rows, float scale, void* workspace_dev, void* stream);
+
+/*
  * Test hook for the bounded wait of the kernels that stage their inputs with asynchronous
  * copies.  The next step launched by this process announces 16 bytes more than it copies for
  * the inputs of tile number `tile` (tiles of 2048 elements, counted over the tensor list), so the

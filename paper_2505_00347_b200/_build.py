@@ -26,6 +26,7 @@ UNITS = [
     ("solo_api.cu", "solo_api.o", []),
     ("solo_dispatch.cu", "solo_dispatch.o", []),
     ("solo_grad.cu", "solo_grad.o", []),
+    ("solo_grad_rows.cu", "solo_grad_rows.o", []),
     ("solo_step_inst.cu", "solo_step_bm2.o", ["-DSOLO_BM=2"]),
     ("solo_step_inst.cu", "solo_step_bm3.o", ["-DSOLO_BM=3"]),
     ("solo_step_inst.cu", "solo_step_bm4.o", ["-DSOLO_BM=4"]),

@@ -74,6 +74,16 @@ class GradList(C.Structure):
     _fields_ = [("grads", C.c_void_p), ("data", C.c_void_p), ("dtype", C.c_int32)]
 
 
+class GradRows(C.Structure):
+    """solo_grad_rows_t"""
+
+    _fields_ = [
+        ("acc", C.c_void_p), ("num_rows", C.c_int64), ("width", C.c_int64), ("tokens", C.c_void_p),
+        ("token_bytes", C.c_int32), ("grad_dtype", C.c_int32), ("grad", C.c_void_p), ("grad_stride", C.c_int64),
+        ("num_tokens", C.c_int64),
+    ]
+
+
 def hyper(lr=1e-3, beta1=0.8, beta2=0.999, eps=1e-8, weight_decay=0.01, p_quantile=0.1,
           adamw=1, bias_correction=1, round_m=0, round_v=1, param_dtype=0, seed=0, belief=0, fixed_alpha=0.0,
           param_round=0, v_codebook=0) -> Hyper:
@@ -142,6 +152,8 @@ def lib() -> C.CDLL:
     L.solo_grad_clip.argtypes = [gl, gl, vp, i32, i32, f32, f32, vp]
     L.solo_grad_clip_norm.argtypes = [gl, gl, i32, f32, f32, vp, vp, vp, vp]
     L.solo_grad_accumulate.argtypes = [gl, gl, f32, i32, i32, vp, vp, vp, vp]
+    L.solo_grad_rows_workspace.argtypes = [i64, i64, C.POINTER(C.c_size_t)]
+    L.solo_grad_accumulate_rows.argtypes = [C.POINTER(GradRows), f32, vp, vp]
     L.solo_strerror.restype = C.c_char_p
     for name in ("solo_state_create", "solo_state_create_multi", "solo_state_destroy",
                  "solo_state_bytes", "solo_step", "solo_multi_step", "solo_dequant",
@@ -149,7 +161,7 @@ def lib() -> C.CDLL:
                  "solo_set_kernel_policy", "solo_debug_check_fast_log", "solo_state_export_bytes",
                  "solo_state_export", "solo_state_import", "solo_grads_create", "solo_grads_destroy",
                  "solo_grads_workspace", "solo_grad_norm", "solo_grad_clip", "solo_grad_clip_norm",
-                 "solo_grad_accumulate"):
+                 "solo_grad_accumulate", "solo_grad_rows_workspace", "solo_grad_accumulate_rows"):
         getattr(L, name).restype = C.c_int
     _lib = L
     return L
@@ -522,6 +534,41 @@ def solo_grad_accumulate(acc: GradSet, grads: GradSet, scale: float = 1.0, first
     if rc:
         _check(rc, "solo_grad_accumulate")
     return _norm_results(ws, acc, per_tensor)
+
+_TOKEN_BYTES = {torch.int32: 4, torch.int64: 8}
+
+
+def solo_grad_accumulate_rows(acc: torch.Tensor, tokens: torch.Tensor, grad: torch.Tensor, scale: float = 1.0) -> None:
+    """acc[tokens[i], :] += scale * grad[i, :], the gradient of an embedding.  acc: fp32 [rows, width], contiguous; tokens:
+    int32 or int64 of any shape, contiguous; grad: fp32, bf16 or fp16 of that shape and a last dimension of width, contiguous
+    or, with one dimension of tokens, with rows any distance apart.  Tokens outside the table contribute nothing."""
+    if acc.dim() != 2 or acc.dtype != torch.float32 or not acc.is_contiguous() or not acc.is_cuda:
+        raise ValueError("acc must be a contiguous float32 CUDA matrix")
+    num_rows, width = acc.shape
+    if tokens.dtype not in _TOKEN_BYTES or not tokens.is_contiguous() or tokens.device != acc.device:
+        raise ValueError("tokens must be contiguous int32 or int64 on the accumulator's device")
+    if grad.dtype not in _GRAD_DTYPE or grad.device != acc.device or grad.shape != (*tokens.shape, width):
+        raise ValueError("grad must be fp32, bf16 or fp16 of the tokens' shape and the accumulator's width, on its device")
+    if acc.device.index != torch.cuda.current_device():
+        raise ValueError("tensors must be on the current device")
+    n = tokens.numel()
+    if grad.is_contiguous():
+        stride = width
+    elif grad.dim() == 2 and (width == 1 or grad.stride(1) == 1):
+        stride = grad.stride(0)
+    else:
+        raise ValueError("grad must be contiguous, or a matrix with contiguous rows")
+    if n == 0 or num_rows == 0 or width == 0:
+        return
+    L = _lib or lib()
+    size = C.c_size_t()
+    _check(L.solo_grad_rows_workspace(n, width, C.byref(size)), "solo_grad_rows_workspace")
+    ws = torch.empty(size.value, dtype=torch.uint8, device=acc.device)
+    desc = GradRows(acc.data_ptr(), num_rows, width, tokens.data_ptr(), _TOKEN_BYTES[tokens.dtype], _GRAD_DTYPE[grad.dtype],
+                    grad.data_ptr(), stride, n)
+    rc = L.solo_grad_accumulate_rows(C.byref(desc), scale, ws.data_ptr(), _stream())
+    if rc:
+        _check(rc, "solo_grad_accumulate_rows")
 
 
 def codebook_m(bits: int) -> torch.Tensor:

@@ -51,3 +51,27 @@ def test_python_checks_come_before_the_library(B):
         with pytest.raises(ValueError):
             B._norm_type(p)
     assert (B._norm_type(2.0), B._norm_type(1), B._norm_type(float("inf"))) == (2, 1, 0)
+
+
+def test_rows_are_checked(B):
+    L, n = B.lib(), C.c_size_t()
+    for tokens, width in ((-1, 8), (1, 0), (1, (1 << 24) + 1), ((1 << 40) + 1, 8)):
+        assert L.solo_grad_rows_workspace(tokens, width, C.byref(n)) == B.SOLO_EINVAL
+    assert L.solo_grad_rows_workspace(5, 8, None) == B.SOLO_EINVAL
+    assert L.solo_grad_rows_workspace(0, 8, C.byref(n)) == B.SOLO_OK
+    sizes = []
+    for tokens in (1, 64, 1000, 65536, 65537, 1 << 40):
+        assert L.solo_grad_rows_workspace(tokens, 768, C.byref(n)) == B.SOLO_OK
+        sizes.append(n.value)
+    assert sizes == sorted(sizes) and sizes[-1] == sizes[-3]              # one chunk's workspace serves all
+
+    good = dict(acc=256, num_rows=5, width=8, tokens=256, token_bytes=8, grad_dtype=0, grad=256, grad_stride=8, num_tokens=3)
+    call = lambda ws=256, scale=1.0, **kw: L.solo_grad_accumulate_rows(C.byref(B.GradRows(*{**good, **kw}.values())), scale, ws, None)  # noqa: E731
+    for kw in (dict(acc=None), dict(num_rows=0), dict(num_rows=1 << 31), dict(width=0), dict(width=(1 << 24) + 1), dict(tokens=None),
+               dict(token_bytes=2), dict(grad_dtype=3), dict(grad_dtype=-1), dict(grad=None), dict(grad_stride=-8), dict(num_tokens=-1),
+               dict(num_tokens=(1 << 40) + 1), dict(ws=None), dict(scale=float("nan")), dict(scale=float("inf"))):
+        assert call(**kw) == B.SOLO_EINVAL, kw
+    for kw in (dict(acc=258), dict(tokens=260), dict(grad=258), dict(ws=264), dict(token_bytes=4, tokens=258)):
+        assert call(**kw) == B.SOLO_EALIGN, kw
+    assert call(num_tokens=0, tokens=None, grad=None, ws=None) == B.SOLO_OK
+    assert L.solo_grad_accumulate_rows(None, 1.0, 256, None) == B.SOLO_EINVAL
