@@ -468,9 +468,9 @@ int solo_grad_accumulate(const solo_grad_list_t* acc, const solo_grad_list_t* gr
 /*
  * The gradient of an embedding, added to its accumulator: acc[tokens[i], :] += scale * grad[i, :], i = 0 .. num_tokens - 1.
  * Tokens outside [0, num_rows) (padding, masked positions) contribute nothing, whatever their rows hold; rows of acc that no
- * token names stay as they are.  The rows of one token are summed in their order, in pieces of fewer than 96 in binary32 and over
- * the pieces in binary64, for 65,536 tokens at a time, and each such sum is added with one rounding: the same inputs
- * give the same bits.
+ * token names stay as they are.  The rows of one token are summed in binary32, 16 and then 8 of these sums at a time, and in binary64
+ * beyond, for 65,536 tokens together; each such sum is added with one rounding.  The order depends on the tokens alone:
+ * the same inputs give the same bits.
  */
 typedef struct {
     float* acc;                  /* device [num_rows, width], binary32 */

@@ -1,11 +1,12 @@
 // The gradient of an embedding, added to its fp32 accumulator: acc[tok_i, :] += s * g[i, :] (include/solo.h).
 //
 // Two launches for up to 65,536 tokens.  A cluster of up to eight CTAs sorts the tokens with their positions in its shared memory
-// (least significant digit first, stable, so that equal tokens keep their order); then every warp takes a window of the sorted
-// order and 256 columns, sums the rows of each run of equal tokens in registers and adds the sum to the accumulator's row, which so
-// is read and written once, without atomics and in an order that the tokens alone decide.  A window holds about the same number of rows
-// whatever the tokens are, so that frequent ones cost no more than rare ones.  Long runs are cut at window starts; the
-// pieces' sums go to the workspace, and the warp that finishes last adds them up in their order.
+// (least significant digit first, stable, so that equal tokens keep their order); then a CTA takes 128 entries of the sorted
+// order and 256 columns, a warp 16 of these entries.  A warp sums the rows of each run of equal tokens in registers; runs that
+// lie in one warp's entries are added to the accumulator at once, the pieces of others are put together in shared memory, and those of
+// runs that reach into other CTAs in the workspace, by the CTA that finishes last, in their order.  So every row of the
+// accumulator is read and written once, without atomics and in an order that the tokens alone decide, and a CTA has the
+// same number of rows whatever the tokens are: frequent ones cost no more than rare ones.
 #include "solo.h"
 
 #include <cooperative_groups.h>
@@ -34,8 +35,9 @@ constexpr int SORT_SMALL = 2048;                       // tokens per CTA that th
 constexpr int CHUNK = SORT_CLUSTER * SORT_PER_CTA;     // tokens per pair of launches
 constexpr int DIGIT_MIN = 5, DIGIT_MAX = 9, DIGITS = 1 << DIGIT_MAX;
 
-constexpr int WINDOW = 32, WINDOW_BACK = 16;           // entries of a warp; where runs are cut, see rows_sum_kernel
-constexpr int ROWS_CTA = 256, SLAB = 256;              // threads of the summing kernel; columns of a warp
+constexpr int ROWS_WARPS = 8, ROWS_CTA = ROWS_WARPS * 32;   // of the summing kernel
+constexpr int WARP_ROWS = 16, CTA_ROWS = ROWS_WARPS * WARP_ROWS;
+constexpr int SLAB = 256;                              // columns of a CTA
 
 struct SortArgs {
     const void* tokens;
@@ -51,7 +53,8 @@ struct SortArgs {
 struct SortShared {
     uint2 item[2][SORT_PER_CTA];                // token, position
     uint16_t hist[SORT_WARPS * DIGITS];         // [warp][digit] of each warp, then how many of a digit lie in the warps before
-    uint32_t part[SORT_CTA];                    // [group of warps][digit]
+    uint32_t part[SORT_CTA];                    // [group of warps][digit]: how many
+    uint32_t before[SORT_CTA];                  // the same: how many in the groups before
     uint32_t total[SORT_CLUSTER][DIGITS];       // of each CTA
     uint32_t base[DIGITS];                      // first place of a digit's tokens of this CTA
     uint32_t scan[SORT_WARPS];
@@ -94,7 +97,14 @@ __global__ __launch_bounds__(SORT_CTA) void rows_sort_kernel(const __grid_consta
                 const bool have = j < count;
                 item[r] = have ? s.item[from][j] : make_uint2(0, 0);
                 const int d = have ? (int)((item[r].x >> shift) & (uint32_t)(digits - 1)) : digits;
-                const uint32_t peers = __match_any_sync(0xFFFFFFFFu, d);
+                // Lanes with the same digit, a vote for each of its bits (a match over the warp takes a step per distinct
+                // digit: 2000 cycles a round where this takes 300).
+                uint32_t peers = __ballot_sync(0xFFFFFFFFu, have);
+                for (int b = 0; b < a.digit_bits; ++b) {
+                    const bool bit = (d >> b) & 1;
+                    const uint32_t vote = __ballot_sync(0xFFFFFFFFu, bit);
+                    peers &= bit ? vote : ~vote;
+                }
                 const uint32_t before = peers & ((1u << lane) - 1u);
                 rank[r] = have ? hist[d] + __popc(before) : 0xFFFFFFFFu;
                 __syncwarp();
@@ -117,10 +127,9 @@ __global__ __launch_bounds__(SORT_CTA) void rows_sort_kernel(const __grid_consta
             if (g < group) before_group += v;
             total += v;
         }
+        s.before[tid] = before_group;
         if (group == 0)
             for (int r = 0; r < ctas; ++r) cluster.map_shared_rank(&s, r)->total[me][digit] = total;
-        for (int w = group * group_warps; w < (group + 1) * group_warps; ++w)
-            s.hist[w * digits + digit] = (uint16_t)(s.hist[w * digits + digit] + before_group);
         cluster.sync();
         // Digits before this one in the whole cluster, then the CTAs before this one.
         uint32_t all = 0, mine = 0, upto = 0;
@@ -148,7 +157,7 @@ __global__ __launch_bounds__(SORT_CTA) void rows_sort_kernel(const __grid_consta
         for (int r = 0; r < SORT_ROUNDS; ++r) {
             if (r < rounds && rank[r] != 0xFFFFFFFFu) {
                 const int d = (int)((item[r].x >> shift) & (uint32_t)(digits - 1));
-                const uint32_t to = s.base[d] + hist[d] + rank[r];
+                const uint32_t to = s.base[d] + s.before[(warp / group_warps << a.digit_bits) + d] + hist[d] + rank[r];
                 cluster.map_shared_rank(&s, to >> a.log_per_cta)->item[from ^ 1][to & (uint32_t)(per_cta - 1)] = item[r];
             }
         }
@@ -167,8 +176,8 @@ struct RowsArgs {
     const void* grad;
     const uint32_t* tok;
     const uint16_t* pos;
-    float* partial;             // [2 windows, width]: pieces that start with a window, then runs' first pieces, at the first cut
-    uint32_t* counters;         // [windows, slabs] pieces done, at a run's first cut
+    float* partial;             // [2 CTAs, width]: pieces that continue a run, then runs' first pieces
+    uint32_t* counters;         // [CTAs, slabs] pieces done, at a run's first CTA
     int64_t width, grad_stride;
     int32_t num_tokens, num_rows, slabs;
     float scale;
@@ -248,142 +257,160 @@ template <int DT, bool VEC> struct Cols {
     }
 };
 
-// First and last + 1 entry of token t: half a warp each, sixteen places at a time.
-__device__ __forceinline__ void run_bounds(const uint32_t* tok, int n, uint32_t t, int& begin, int& end) {
-    const int lane = threadIdx.x & 31, half = lane >> 4, place = lane & 15;
-    int lo = -1, hi = n;                       // tok[lo] < target <= tok[hi]
-    while (__any_sync(0xFFFFFFFFu, hi - lo > 1)) {
-        const int step = (hi - lo + 15) / 16;
-        const int probe = lo + (place + 1) * step;
-        const bool below = probe < hi && tok[probe] < t + half;
-        const uint32_t b = __ballot_sync(0xFFFFFFFFu, below);
-        lo += __popc(half ? b >> 16 : b & 0xFFFFu) * step;
-        hi = min(hi, lo + step);
+// What the CTAs and warps before and after do is known from the tokens next to their borders.
+__device__ __forceinline__ int ctas_before(const uint32_t* tok, int c, uint32_t t) {       // that a run reaches back into from CTA c
+    int k = 0;
+    for (;;) {
+        const int e = (c - k - (int)(threadIdx.x & 31)) * CTA_ROWS - 1;
+        const uint32_t same = __ballot_sync(0xFFFFFFFFu, e >= 0 && tok[e] == t);
+        if (same != 0xFFFFFFFFu) return k + __ffs(~same) - 1;
+        k += 32;
     }
-    begin = __shfl_sync(0xFFFFFFFFu, hi, 0);
-    end = __shfl_sync(0xFFFFFFFFu, hi, 16);
+}
+__device__ __forceinline__ int ctas_after(const uint32_t* tok, int n, int c, uint32_t t) {  // that it reaches on into
+    int k = 0;
+    for (;;) {
+        const int64_t e = (int64_t)(c + 1 + k + (int)(threadIdx.x & 31)) * CTA_ROWS;
+        const uint32_t same = __ballot_sync(0xFFFFFFFFu, e < n && tok[e] == t);
+        if (same != 0xFFFFFFFFu) return k + __ffs(~same) - 1;
+        k += 32;
+    }
 }
 
-// A warp sums the runs that start in its window, and a run that was cut at its start, over its 256 columns.  A run is cut
-// at a window's start if it began WINDOW_BACK entries before or earlier, so that short runs are never cut and a warp
-// reaches into the next window, but not beyond.
+struct SumShared {
+    union {
+        float open[2][ROWS_WARPS][8][32];       // pieces of runs that a warp does not hold whole: what continues one, what begins one
+        double join[ROWS_WARPS][8][32];
+    };
+    uint32_t head[ROWS_WARPS];                  // 0: the warp's first run is its own; 1: continues one and ends here; 2: goes on
+    int32_t job[2][2];                          // runs to put together: first CTA (-1: none), CTAs after it
+    uint32_t job_tok[2];
+};
+
 template <int DT, bool VEC> __global__ __launch_bounds__(ROWS_CTA) void rows_sum_kernel(const __grid_constant__ RowsArgs a) {
     constexpr uint32_t ALL = 0xFFFFFFFFu, NONE = 0xFFFFFFFFu;
+    __shared__ SumShared s;
     pdl_wait();
     pdl_release();
-    const int lane = threadIdx.x & 31;
-    const int n = a.num_tokens, windows = (n + WINDOW - 1) / WINDOW;
-    const int64_t task = (int64_t)blockIdx.x * (ROWS_CTA / 32) + (threadIdx.x >> 5);
-    const int w = (int)(task / a.slabs), slab = (int)(task % a.slabs);
-    if (w >= windows) return;
-    const int base = w * WINDOW, next = base + WINDOW;
-    const uint32_t t0 = base + lane < n ? a.tok[base + lane] : NONE;
-    const uint32_t t1 = next + lane < n ? a.tok[next + lane] : NONE;
-    const int p0 = base + lane < n ? a.pos[base + lane] : 0;
-    const int p1 = next + lane < n ? a.pos[next + lane] : 0;
-    const uint32_t before = base > 0 ? a.tok[base - 1] : NONE;
-    const uint32_t back = base > 0 ? a.tok[base - WINDOW_BACK] : NONE;
-    const uint32_t beyond = next + WINDOW < n ? a.tok[next + WINDOW] : NONE;
-    uint32_t prev = __shfl_up_sync(ALL, t0, 1);
-    if (lane == 0) prev = before;
-    const uint32_t rows = (uint32_t)a.num_rows;
-    const uint32_t firsts = __ballot_sync(ALL, t0 != prev && t0 < rows);                  // entries that begin a run
-    const bool cut0 = t0 == back;                                                         // (lane 0's is used)
-    const uint32_t starts = firsts | (__ballot_sync(ALL, lane == 0 && cut0 && t0 < rows));
-    if (starts == 0) return;
-    const int inside = __popc(__ballot_sync(ALL, t0 < rows));                            // tokens outside come last
-    int total = inside;
-    bool last_cut = false;
-    if (inside == WINDOW) {
-        const uint32_t t = __shfl_sync(ALL, t0, WINDOW - 1);
-        if (__shfl_sync(ALL, t1, 0) == t) {
-            last_cut = __shfl_sync(ALL, t0, WINDOW - WINDOW_BACK) == t;
-            if (!last_cut) {
-                const uint32_t same = __ballot_sync(ALL, t1 == t);
-                total += same == ALL ? WINDOW : __ffs(~same) - 1;
-                last_cut = same == ALL && beyond == t;
-            }
-        }
-    }
-    const bool first_cut = (firsts & 1u) == 0 && (starts & 1u);                           // the first piece continues a run
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int n = a.num_tokens, c = (int)(blockIdx.x / (unsigned)a.slabs), slab = (int)(blockIdx.x % (unsigned)a.slabs);
+    const int first_of_second = (n + CTA_ROWS - 1) / CTA_ROWS;          // CTAs over the entries: where first pieces start in `partial`
+    const int base = c * CTA_ROWS + warp * WARP_ROWS;
+    // This warp's entries and one on either side; tokens outside the table come last and count as none.
+    const int e = base - 1 + lane;
+    uint32_t around = lane < WARP_ROWS + 2 && e >= 0 && e < n ? a.tok[e] : NONE;
+    if (around >= (uint32_t)a.num_rows) around = NONE;
+    const int pos = lane < WARP_ROWS && base + lane < n ? a.pos[base + lane] : 0;
+    const uint32_t tok = __shfl_down_sync(ALL, around, 1), next = __shfl_down_sync(ALL, around, 2);
+    const bool valid = lane < WARP_ROWS && tok != NONE;
+    const uint32_t starts = __ballot_sync(ALL, valid && tok != around), ends = __ballot_sync(ALL, valid && tok != next);
+    const int count = __popc(__ballot_sync(ALL, valid));
+    const bool continues = count > 0 && !(starts & 1u);                 // the first run began before this warp
+    const bool goes_on = count > 0 && !(ends >> (count - 1) & 1u);      // the last run ends after it
+    const bool through = continues && goes_on && ends == 0;             // and these are one
     Cols<DT, VEC> cols;
     cols.width = a.width;
     cols.c0 = (int64_t)slab * SLAB + (VEC ? lane * 8 : lane);
+    if (threadIdx.x < 2) s.job[threadIdx.x][0] = -1;
+    if (lane == 0) s.head[warp] = continues ? (through ? 2 : 1) : 0;
     float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     constexpr int BATCH = 4;
-    const int begin = __ffs(starts) - 1;
-    int piece = begin;                                                                    // first entry of the piece summed
-    for (int k = begin; k < total; k += BATCH) {
+    for (int k = 0; k < count; k += BATCH) {
         typename Cols<DT, VEC>::Raw r[BATCH];
         float v[BATCH][8];
-        bool ends[BATCH];
         float* row[BATCH];
+        bool whole[BATCH];                                              // entry that ends a run of this warp alone
 #pragma unroll
         for (int b = 0; b < BATCH; ++b) {
             const int x = k + b;
-            const int pa = __shfl_sync(ALL, p0, x & 31), pb = __shfl_sync(ALL, p1, x & 31);
-            const uint32_t t = __shfl_sync(ALL, t0, min(x, WINDOW - 1));
-            ends[b] = x == total - 1 || (x < WINDOW - 1 && (starts >> (x + 1)) & 1u);
-            row[b] = a.acc + (int64_t)t * a.width;
-            if (x < total) {
-                r[b] = cols.load(a.grad, (x < WINDOW ? pa : pb) * a.grad_stride);
-                if (ends[b]) cols.load_f32(row[b], v[b]);
+            const int p = __shfl_sync(ALL, pos, x);
+            row[b] = a.acc + (int64_t)__shfl_sync(ALL, tok, x) * a.width;
+            whole[b] = (ends >> x & 1u) && !(continues && (ends & ((1u << x) - 1u)) == 0);
+            if (x < count) {
+                r[b] = cols.load(a.grad, p * a.grad_stride);
+                if (whole[b]) cols.load_f32(row[b], v[b]);
             }
         }
 #pragma unroll
         for (int b = 0; b < BATCH; ++b) {
             const int x = k + b;
-            if (x < total) {
+            if (x < count) {
                 cols.add(r[b], sum);
-                if (ends[b]) {
-                    if ((first_cut && piece == 0) || (last_cut && x == total - 1)) {
-                        // a run's first piece lies at its first cut: the next window's start, or the one after if it is the last one's end
-                        const int slot = first_cut && piece == 0 ? w : windows + w + (total > WINDOW ? 2 : 1);
-                        cols.store_f32(a.partial + (int64_t)slot * a.width, sum);
-                    } else {
+                if ((ends >> x & 1u) || x == count - 1) {
+                    if (whole[b]) {
 #pragma unroll
                         for (int q = 0; q < 8; ++q) v[b][q] = __fmaf_rn(a.scale, sum[q], v[b][q]);
                         cols.store_f32(row[b], v[b]);
+                    } else {
+                        const int which = continues && (ends & ((1u << x) - 1u)) == 0 ? 0 : 1;
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) s.open[which][warp][q][lane] = sum[q];
                     }
 #pragma unroll
                     for (int q = 0; q < 8; ++q) sum[q] = 0.0f;
-                    piece = x + 1;
                 }
             }
         }
     }
-    if (!first_cut && !last_cut) return;
-    __threadfence();
-    __syncwarp();
-    // Of a run that is cut on both sides of this window there is one piece here.
-    const bool one = first_cut && last_cut && (starts & (starts - 1)) == 0;
+    __syncthreads();
+    // Runs of several warps, by the warp that holds the first piece: in this CTA, or (warp 0) of a run from a CTA before.
     for (int side = 0; side < 2; ++side) {
-        if (side == 0 ? !first_cut : !last_cut || one) continue;
-        const uint32_t t = __shfl_sync(ALL, t0, side == 0 ? 0 : WINDOW - 1);
-        int from, to;
-        run_bounds(a.tok, n, t, from, to);
-        const int cut = (from + WINDOW_BACK + WINDOW - 1) / WINDOW;                       // window of the run's first cut
-        const int last = (to - 1) / WINDOW;                                               // window of its last entry
-        uint32_t done = 0;
-        if (lane == 0) done = atomicAdd(&a.counters[(int64_t)cut * a.slabs + slab], 1u);
-        if (__shfl_sync(ALL, done, 0) != (uint32_t)(last - cut + 1)) continue;            // the first piece and one for each window
-        __threadfence();
-        float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        double d[8];
-        cols.load_f32(a.partial + (int64_t)(windows + cut) * a.width, v);
+        if (side == 0 ? !(warp == 0 && continues) : !(goes_on && !through)) continue;
+        bool open = side == 1 || through;
+        float v[8];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) d[q] = (double)v[q];
+        for (int q = 0; q < 8; ++q) v[q] = s.open[side][warp][q][lane];
+        for (int u = warp + 1; open && u < ROWS_WARPS; ++u) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v[q] += s.open[0][u][q][lane];
+            open = s.head[u] == 2;
+        }
+        const uint32_t t = __shfl_sync(ALL, tok, side == 0 ? 0 : WARP_ROWS - 1);
+        if (side == 1 && !open) {
+            float* const row = a.acc + (int64_t)t * a.width;
+            float old[8];
+            cols.load_f32(row, old);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) old[q] = __fmaf_rn(a.scale, v[q], old[q]);
+            cols.store_f32(row, old);
+            continue;
+        }
+        cols.store_f32(a.partial + (int64_t)(side == 0 ? c : first_of_second + c) * a.width, v);
+        const int from = side == 0 ? c - ctas_before(a.tok, c, t) : c;
+        const int to = open ? c + ctas_after(a.tok, n, c, t) : c;
+        __threadfence();
+        __syncwarp();
+        if (lane == 0 && atomicAdd(&a.counters[(int64_t)from * a.slabs + slab], 1u) == (uint32_t)(to - from)) {
+            s.job[side][0] = from;
+            s.job[side][1] = to - from;
+            s.job_tok[side] = t;
+        }
+    }
+    __syncthreads();
+    for (int side = 0; side < 2; ++side) {
+        const int from = s.job[side][0], more = s.job[side][1];
+        if (from < 0) continue;
+        __threadfence();
+        double d[8] = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll 4
-        for (int p = cut; p <= last; ++p) {
-            cols.load_f32(a.partial + (int64_t)p * a.width, v);
+        for (int p = warp; p <= more; p += ROWS_WARPS) {
+            float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+            cols.load_f32(a.partial + (int64_t)(p == 0 ? first_of_second + from : from + p) * a.width, v);
 #pragma unroll
             for (int q = 0; q < 8; ++q) d[q] += (double)v[q];
         }
-        float* const row = a.acc + (int64_t)t * a.width;
-        cols.load_f32(row, v);
+        __syncthreads();                                                // of the other side's sums
 #pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] = __fmaf_rn(a.scale, (float)d[q], v[q]);
-        cols.store_f32(row, v);
+        for (int q = 0; q < 8; ++q) s.join[warp][q][lane] = d[q];
+        __syncthreads();
+        double all = 0.0;
+#pragma unroll
+        for (int u = 0; u < ROWS_WARPS; ++u) all += s.join[u][warp][lane];
+        const int64_t col = (int64_t)slab * SLAB + (VEC ? lane * 8 + warp : warp * 32 + lane);
+        if (col < a.width) {
+            float* const at = a.acc + (int64_t)s.job_tok[side] * a.width + col;
+            *at = __fmaf_rn(a.scale, (float)all, *at);
+        }
     }
 }
 
@@ -441,13 +468,13 @@ size_t pad256(size_t n) { return (n + 255) / 256 * 256; }
 
 RowsLayout rows_layout(int64_t num_tokens, int64_t width) {
     RowsLayout l;
-    const int64_t n = std::min<int64_t>(num_tokens, CHUNK), windows = (n + WINDOW - 1) / WINDOW;
+    const int64_t n = std::min<int64_t>(num_tokens, CHUNK), ctas = (n + CTA_ROWS - 1) / CTA_ROWS;
     l.slabs = (width + SLAB - 1) / SLAB;
     l.tok = 0;
     l.pos = l.tok + pad256((size_t)n * 4);
     l.counters = l.pos + pad256((size_t)n * 2);
-    l.partial = l.counters + pad256((size_t)(windows * l.slabs) * 4);
-    l.total = l.partial + pad256((size_t)(2 * windows) * (size_t)width * 4);
+    l.partial = l.counters + pad256((size_t)(ctas * l.slabs) * 4);
+    l.total = l.partial + pad256((size_t)(2 * ctas) * (size_t)width * 4);
     return l;
 }
 
@@ -485,7 +512,8 @@ int solo_grad_accumulate_rows(const solo_grad_rows_t* r, float scale, void* work
     int bits = 1;
     while ((r->num_rows >> bits) != 0) ++bits;                 // the key num_rows stands for tokens outside
     for (int64_t at = 0; at < r->num_tokens; at += CHUNK) {
-        const int n = (int)std::min<int64_t>(CHUNK, r->num_tokens - at), windows = (n + WINDOW - 1) / WINDOW;
+        const int n = (int)std::min<int64_t>(CHUNK, r->num_tokens - at);
+        const int64_t row_ctas = (n + CTA_ROWS - 1) / CTA_ROWS * l.slabs;
         SortArgs s;
         std::memset(&s, 0, sizeof(s));
         s.tokens = (const char*)r->tokens + at * r->token_bytes;
@@ -497,7 +525,7 @@ int solo_grad_accumulate_rows(const solo_grad_rows_t* r, float scale, void* work
         s.tok = (uint32_t*)(ws + l.tok);
         s.pos = (uint16_t*)(ws + l.pos);
         s.counters = (uint32_t*)(ws + l.counters);
-        s.num_counters = (int32_t)(windows * l.slabs);
+        s.num_counters = (int32_t)row_ctas;
         int ctas = 1;
         while (ctas < SORT_CLUSTER && n > ctas * SORT_SMALL) ctas *= 2;
         while ((ctas << s.log_per_cta) < n) ++s.log_per_cta;
@@ -519,9 +547,7 @@ int solo_grad_accumulate_rows(const solo_grad_rows_t* r, float scale, void* work
         a.slabs = (int32_t)l.slabs;
         a.scale = scale;
         void* rp[] = {&a};
-        const int64_t warps = windows * l.slabs;
-        rc = launch((const void*)rows_kernel_for(r->grad_dtype, vec), dim3((unsigned)((warps + ROWS_CTA / 32 - 1) / (ROWS_CTA / 32))), ROWS_CTA, 0, 0,
-                    rp, stream);
+        rc = launch((const void*)rows_kernel_for(r->grad_dtype, vec), dim3((unsigned)row_ctas), ROWS_CTA, 0, 0, rp, stream);
         if (rc != SOLO_OK) return rc;
     }
     return SOLO_OK;
