@@ -468,9 +468,9 @@ int solo_grad_accumulate(const solo_grad_list_t* acc, const solo_grad_list_t* gr
 /*
  * The gradient of an embedding, added to its accumulator: acc[tokens[i], :] += scale * grad[i, :], i = 0 .. num_tokens - 1.
  * Tokens outside [0, num_rows) (padding, masked positions) contribute nothing, whatever their rows hold; rows of acc that no
- * token names stay as they are.  The rows of one token are summed in binary32, 16 and then 8 of these sums at a time, and in binary64
- * beyond, for 65,536 tokens together; each such sum is added with one rounding.  The order depends on the tokens alone:
- * the same inputs give the same bits.
+ * token names stay as they are.  The rows of one token are summed in binary32 in groups (fewer than 48 additions follow one another) and
+ * the groups in binary64, for 65,536 tokens together; each such sum is added with one rounding.  The order depends on the
+ * tokens alone: the same inputs give the same bits.
  */
 typedef struct {
     float* acc;                  /* device [num_rows, width], binary32 */
@@ -483,7 +483,7 @@ typedef struct {
     int64_t grad_stride;         /* >= 0 */
     int64_t num_tokens;          /* 0 .. 2^40 */
 } solo_grad_rows_t;
-/* `workspace_dev`: 16-byte aligned device memory of solo_grad_rows_workspace's size, as for solo_grads_workspace. */
+/* `workspace_dev`: 16-byte aligned device memory of solo_grad_rows_workspace's size, as for solo_grads_workspace; NULL if that is 0. */
 int solo_grad_rows_workspace(int64_t num_tokens, int64_t width, size_t* bytes);
 int solo_grad_accumulate_rows(const solo_grad_rows_t* rows, float scale, void* workspace_dev, void* stream);
 

@@ -563,10 +563,10 @@ def solo_grad_accumulate_rows(acc: torch.Tensor, tokens: torch.Tensor, grad: tor
     L = _lib or lib()
     size = C.c_size_t()
     _check(L.solo_grad_rows_workspace(n, width, C.byref(size)), "solo_grad_rows_workspace")
-    ws = torch.empty(size.value, dtype=torch.uint8, device=acc.device)
+    ws = torch.empty(size.value, dtype=torch.uint8, device=acc.device) if size.value else None
     desc = GradRows(acc.data_ptr(), num_rows, width, tokens.data_ptr(), _TOKEN_BYTES[tokens.dtype], _GRAD_DTYPE[grad.dtype],
                     grad.data_ptr(), stride, n)
-    rc = L.solo_grad_accumulate_rows(C.byref(desc), scale, ws.data_ptr(), _stream())
+    rc = L.solo_grad_accumulate_rows(C.byref(desc), scale, ws.data_ptr() if size.value else None, _stream())
     if rc:
         _check(rc, "solo_grad_accumulate_rows")
 

@@ -7,6 +7,9 @@
 // runs that reach into other CTAs in the workspace, by the CTA that finishes last, in their order.  So every row of the
 // accumulator is read and written once, without atomics and in an order that the tokens alone decide, and a CTA has the
 // same number of rows whatever the tokens are: frequent ones cost no more than rare ones.
+//
+// A few tokens take one launch: a CTA per token and 256 columns looks for the same token in the whole list and, if its
+// own is the first, sums the rows.
 #include "solo.h"
 
 #include <cooperative_groups.h>
@@ -100,7 +103,8 @@ __global__ __launch_bounds__(SORT_CTA) void rows_sort_kernel(const __grid_consta
                 // Lanes with the same digit, a vote for each of its bits (a match over the warp takes a step per distinct
                 // digit: 2000 cycles a round where this takes 300).
                 uint32_t peers = __ballot_sync(0xFFFFFFFFu, have);
-                for (int b = 0; b < a.digit_bits; ++b) {
+#pragma unroll
+                for (int b = 0; b < DIGIT_MAX; ++b) {
                     const bool bit = (d >> b) & 1;
                     const uint32_t vote = __ballot_sync(0xFFFFFFFFu, bit);
                     peers &= bit ? vote : ~vote;
@@ -114,6 +118,7 @@ __global__ __launch_bounds__(SORT_CTA) void rows_sort_kernel(const __grid_consta
         }
         __syncthreads();
         uint32_t sum = 0;
+#pragma unroll 8
         for (int w = group * group_warps; w < (group + 1) * group_warps; ++w) {
             const uint32_t h = s.hist[w * digits + digit];
             s.hist[w * digits + digit] = (uint16_t)sum;
@@ -414,12 +419,108 @@ template <int DT, bool VEC> __global__ __launch_bounds__(ROWS_CTA) void rows_sum
     }
 }
 
+// One launch for at most DIRECT_MOST tokens.
+constexpr int DIRECT_WORDS = 4;                        // a warp looks at up to four times 32 tokens
+constexpr int DIRECT_MOST = ROWS_WARPS * DIRECT_WORDS * 32;
+
+struct DirectArgs {
+    float* acc;
+    const void* grad;
+    const void* tokens;
+    int64_t width, grad_stride;
+    int32_t token_bytes, num_tokens, num_rows, slabs;
+    float scale;
+};
+
+template <int DT, bool VEC> __global__ __launch_bounds__(ROWS_CTA) void rows_direct_kernel(const __grid_constant__ DirectArgs a) {
+    constexpr uint32_t ALL = 0xFFFFFFFFu;
+    __shared__ float part[ROWS_WARPS][8][32];
+    __shared__ uint32_t found[ROWS_WARPS];             // 1: the token is among the warp's, 2: before this CTA's
+    pdl_wait();
+    pdl_release();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int i = (int)(blockIdx.x / (unsigned)a.slabs), slab = (int)(blockIdx.x % (unsigned)a.slabs);
+    const int n = a.num_tokens, words = (n + ROWS_CTA - 1) / ROWS_CTA;
+    const auto token = [&](int j) { return a.token_bytes == 8 ? ((const int64_t*)a.tokens)[j] : (int64_t)((const int32_t*)a.tokens)[j]; };
+    const int64_t t = token(i);
+    uint32_t m[DIRECT_WORDS];
+    bool before = false;
+#pragma unroll
+    for (int k = 0; k < DIRECT_WORDS; ++k) {
+        const int j = (warp * words + k) * 32 + lane;
+        const bool same = k < words && j < n && token(j) == t;
+        m[k] = __ballot_sync(ALL, same);
+        before |= __any_sync(ALL, same && j < i);
+    }
+    if (t < 0 || t >= a.num_rows) return;
+    const bool have = (m[0] | m[1] | m[2] | m[3]) != 0;
+    if (lane == 0) found[warp] = (have ? 1u : 0u) | (before ? 2u : 0u);
+    __syncthreads();
+    const uint32_t all = __ballot_sync(ALL, lane < ROWS_WARPS && found[lane & (ROWS_WARPS - 1)] & 1u);
+    if (__any_sync(ALL, found[lane & (ROWS_WARPS - 1)] & 2u)) return;
+    const bool alone = (all & (all - 1)) == 0;         // one warp has all the rows
+    if (alone && !have) return;
+    Cols<DT, VEC> cols;
+    cols.width = a.width;
+    cols.c0 = (int64_t)slab * SLAB + (VEC ? lane * 8 : lane);
+    float* const row = a.acc + t * a.width;
+    float old[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (alone) cols.load_f32(row, old);
+    float total[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    constexpr int BATCH = 4;
+#pragma unroll
+    for (int k = 0; k < DIRECT_WORDS; ++k) {
+        float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        uint32_t left = m[k];
+        while (left) {
+            typename Cols<DT, VEC>::Raw r[BATCH];
+            bool on[BATCH];
+#pragma unroll
+            for (int b = 0; b < BATCH; ++b) {
+                on[b] = left != 0;
+                if (on[b]) r[b] = cols.load(a.grad, ((warp * words + k) * 32 + __ffs(left) - 1) * a.grad_stride);
+                left &= left - 1;
+            }
+#pragma unroll
+            for (int b = 0; b < BATCH; ++b)
+                if (on[b]) cols.add(r[b], sum);
+        }
+#pragma unroll
+        for (int q = 0; q < 8; ++q) total[q] += sum[q];
+    }
+    if (alone) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) old[q] = __fmaf_rn(a.scale, total[q], old[q]);
+        cols.store_f32(row, old);
+        return;
+    }
+#pragma unroll
+    for (int q = 0; q < 8; ++q) part[warp][q][lane] = total[q];
+    __syncthreads();
+    const int64_t col = (int64_t)slab * SLAB + (VEC ? lane * 8 + warp : warp * 32 + lane);
+    if (col < a.width) {
+        float v = 0.0f;
+#pragma unroll
+        for (int u = 0; u < ROWS_WARPS; ++u) v += part[u][warp][lane];
+        row[col] = __fmaf_rn(a.scale, v, row[col]);
+    }
+}
+
 using RowsKernel = void (*)(const RowsArgs);
 RowsKernel rows_kernel_for(int dtype, bool vec) {
     switch (dtype) {
         case SOLO_DT_F32: return vec ? rows_sum_kernel<SOLO_DT_F32, true> : rows_sum_kernel<SOLO_DT_F32, false>;
         case SOLO_DT_BF16: return vec ? rows_sum_kernel<SOLO_DT_BF16, true> : rows_sum_kernel<SOLO_DT_BF16, false>;
         default: return vec ? rows_sum_kernel<SOLO_DT_F16, true> : rows_sum_kernel<SOLO_DT_F16, false>;
+    }
+}
+
+using DirectKernel = void (*)(const DirectArgs);
+DirectKernel direct_kernel_for(int dtype, bool vec) {
+    switch (dtype) {
+        case SOLO_DT_F32: return vec ? rows_direct_kernel<SOLO_DT_F32, true> : rows_direct_kernel<SOLO_DT_F32, false>;
+        case SOLO_DT_BF16: return vec ? rows_direct_kernel<SOLO_DT_BF16, true> : rows_direct_kernel<SOLO_DT_BF16, false>;
+        default: return vec ? rows_direct_kernel<SOLO_DT_F16, true> : rows_direct_kernel<SOLO_DT_F16, false>;
     }
 }
 
@@ -466,6 +567,11 @@ struct RowsLayout { size_t tok, pos, counters, partial, total; int64_t slabs; };
 
 size_t pad256(size_t n) { return (n + 255) / 256 * 256; }
 
+// One launch, without a workspace.
+bool rows_direct(int64_t num_tokens, int64_t width) {
+    return num_tokens <= DIRECT_MOST && num_tokens * ((width + SLAB - 1) / SLAB) <= 4096;
+}
+
 RowsLayout rows_layout(int64_t num_tokens, int64_t width) {
     RowsLayout l;
     const int64_t n = std::min<int64_t>(num_tokens, CHUNK), ctas = (n + CTA_ROWS - 1) / CTA_ROWS;
@@ -489,7 +595,7 @@ extern "C" {
 
 int solo_grad_rows_workspace(int64_t num_tokens, int64_t width, size_t* bytes) {
     if (!bytes || num_tokens < 0 || num_tokens > MOST_TOKENS || width < 1 || width > MOST_WIDTH) return SOLO_EINVAL;
-    *bytes = rows_layout(num_tokens, width).total;
+    *bytes = rows_direct(num_tokens, width) ? 0 : rows_layout(num_tokens, width).total;
     return SOLO_OK;
 }
 
@@ -498,17 +604,34 @@ int solo_grad_accumulate_rows(const solo_grad_rows_t* r, float scale, void* work
     if (r->num_tokens < 0 || r->num_tokens > MOST_TOKENS || (r->token_bytes != 4 && r->token_bytes != 8)) return SOLO_EINVAL;
     if (r->grad_dtype < SOLO_DT_F32 || r->grad_dtype > SOLO_DT_F16 || r->grad_stride < 0 || !std::isfinite(scale)) return SOLO_EINVAL;
     if (r->num_tokens == 0) return SOLO_OK;
-    if (!r->tokens || !r->grad || !workspace_dev) return SOLO_EINVAL;
+    const bool direct = rows_direct(r->num_tokens, r->width);
+    if (!r->tokens || !r->grad || (!workspace_dev && !direct)) return SOLO_EINVAL;
     const int es = r->grad_dtype == SOLO_DT_F32 ? 4 : 2;
     if (((uintptr_t)workspace_dev & 15u) || ((uintptr_t)r->acc & 3u) || ((uintptr_t)r->tokens & (unsigned)(r->token_bytes - 1)) ||
         ((uintptr_t)r->grad & (unsigned)(es - 1)))
         return SOLO_EALIGN;
+    cudaStream_t stream = (cudaStream_t)stream_;
+    const bool vec = r->width % 8 == 0 && (((uintptr_t)r->acc | (uintptr_t)r->grad) & 15u) == 0 && (r->grad_stride * es) % 16 == 0;
+    const RowsLayout l = rows_layout(r->num_tokens, r->width);
+    if (direct) {
+        DirectArgs d;
+        std::memset(&d, 0, sizeof(d));
+        d.acc = r->acc;
+        d.grad = r->grad;
+        d.tokens = r->tokens;
+        d.width = r->width;
+        d.grad_stride = r->grad_stride;
+        d.token_bytes = r->token_bytes;
+        d.num_tokens = (int32_t)r->num_tokens;
+        d.num_rows = (int32_t)r->num_rows;
+        d.slabs = (int32_t)l.slabs;
+        d.scale = scale;
+        void* dp[] = {&d};
+        return launch((const void*)direct_kernel_for(r->grad_dtype, vec), dim3((unsigned)(r->num_tokens * l.slabs)), ROWS_CTA, 0, 0, dp, stream);
+    }
     int rc = sort_ready();
     if (rc != SOLO_OK) return rc;
-    cudaStream_t stream = (cudaStream_t)stream_;
-    const RowsLayout l = rows_layout(r->num_tokens, r->width);
     unsigned char* ws = (unsigned char*)workspace_dev;
-    const bool vec = r->width % 8 == 0 && (((uintptr_t)r->acc | (uintptr_t)r->grad) & 15u) == 0 && (r->grad_stride * es) % 16 == 0;
     int bits = 1;
     while ((r->num_rows >> bits) != 0) ++bits;                 // the key num_rows stands for tokens outside
     for (int64_t at = 0; at < r->num_tokens; at += CHUNK) {

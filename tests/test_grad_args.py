@@ -60,7 +60,7 @@ def test_rows_are_checked(B):
     assert L.solo_grad_rows_workspace(5, 8, None) == B.SOLO_EINVAL
     assert L.solo_grad_rows_workspace(0, 8, C.byref(n)) == B.SOLO_OK
     sizes = []
-    for tokens in (1, 64, 1000, 65536, 65537, 1 << 40):
+    for tokens in (1, 64, 2000, 65536, 65537, 1 << 40):
         assert L.solo_grad_rows_workspace(tokens, 768, C.byref(n)) == B.SOLO_OK
         sizes.append(n.value)
     assert sizes == sorted(sizes) and sizes[-1] == sizes[-3]              # one chunk's workspace serves all
@@ -69,7 +69,7 @@ def test_rows_are_checked(B):
     call = lambda ws=256, scale=1.0, **kw: L.solo_grad_accumulate_rows(C.byref(B.GradRows(*{**good, **kw}.values())), scale, ws, None)  # noqa: E731
     for kw in (dict(acc=None), dict(num_rows=0), dict(num_rows=1 << 31), dict(width=0), dict(width=(1 << 24) + 1), dict(tokens=None),
                dict(token_bytes=2), dict(grad_dtype=3), dict(grad_dtype=-1), dict(grad=None), dict(grad_stride=-8), dict(num_tokens=-1),
-               dict(num_tokens=(1 << 40) + 1), dict(ws=None), dict(scale=float("nan")), dict(scale=float("inf"))):
+               dict(num_tokens=(1 << 40) + 1), dict(ws=None, num_tokens=100000), dict(scale=float("nan")), dict(scale=float("inf"))):
         assert call(**kw) == B.SOLO_EINVAL, kw
     for kw in (dict(acc=258), dict(tokens=260), dict(grad=258), dict(ws=264), dict(token_bytes=4, tokens=258)):
         assert call(**kw) == B.SOLO_EALIGN, kw
