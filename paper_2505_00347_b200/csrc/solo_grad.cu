@@ -2,8 +2,10 @@
 //
 // All of these are streams over ragged lists of tensors, a read of 2 or 4 bytes per element and up to
 // 8 bytes written and read besides, and one or two operations on it: bound by HBM.  One kernel template serves them.  The list
-// is cut into tiles of 8192 elements of one tensor each, a CTA takes a contiguous share of the tiles, so that its search
-// for a tensor happens once and its sums need one partial per tensor that it touches.
+// is cut into tiles of 8192 elements of one tensor each.  The CTAs, as many as are resident, take the tiles in turn, so that all
+// of them work on one stretch of memory (clip of the 125M-parameter set 89 -> 79 us against a contiguous share each); where every tensor's
+// norm is wanted a CTA takes a contiguous share instead, so that its sums need one partial for each tensor that it touches.
+// What the next tile is gets looked up while the loads of the present one are under way.
 //
 // Sums.  A thread sums the (at most 32) powers that it takes from a tile in binary32 and adds that to a binary64 sum;
 // threads, CTAs and tensors are summed in binary64 in a fixed order (no atomics), so results do not vary from call to call.
@@ -33,6 +35,7 @@ constexpr int GV = 8;                      // elements per thread and vector: 16
 constexpr int GU = 4;                      // vectors per thread and tile
 constexpr int GTILE = GCTA * GV * GU;      // elements per tile
 constexpr int GCTAS_PER_SM = 8;            // most CTAs per SM that a launch takes (bounds the workspace)
+constexpr int GIN_FLIGHT = 65536;          // bytes of reads per SM that the resident CTAs of a writing pass have under way (pass())
 
 enum { OP_NORM = 0, OP_CLIP = 1, OP_ACC = 2, OP_ACC_FIRST = 3 };
 
@@ -45,6 +48,7 @@ struct GradArgs {
     int32_t num_tensors;
     int32_t norm_type;           // of the factor's norm (OP_CLIP)
     int32_t num_partials, num_norms;
+    int32_t backwards;           // take the list from its end
     float scale, max_norm;
     double* cta_sum;             // [grid] what a CTA's share of the list sums to; null: no norm
     double* slots;               // [grid + T] partial of tensor t from CTA c at c + t: a CTA's last tensor is the next one's
@@ -76,11 +80,22 @@ __device__ __forceinline__ void elem_store(void* p, int64_t i, float v, std::int
 // Eight consecutive elements as they lie in memory.
 template <int DT> struct Raw8 { uint4 q[DT_BYTES<DT> / 2]; };
 
-template <int DT> __device__ __forceinline__ Raw8<DT> load8(const void* p, int64_t i) {
-    const uint4* a = reinterpret_cast<const uint4*>((const char*)p + i * DT_BYTES<DT>);
+// `wide`: fp32 in one access of 32 bytes (accumulation of 809M elements 1439 -> 1284 us against two of 16).
+template <int DT> __device__ __forceinline__ Raw8<DT> load8(const char* p, bool wide) {
+    const uint4* a = reinterpret_cast<const uint4*>(p);
     Raw8<DT> r;
-#pragma unroll
-    for (int k = 0; k < DT_BYTES<DT> / 2; ++k) r.q[k] = a[k];
+    if constexpr (DT == SOLO_DT_F32) {
+        if (wide) {
+            asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                         : "=r"(r.q[0].x), "=r"(r.q[0].y), "=r"(r.q[0].z), "=r"(r.q[0].w), "=r"(r.q[1].x), "=r"(r.q[1].y), "=r"(r.q[1].z), "=r"(r.q[1].w)
+                         : "l"(a) : "memory");
+        } else {
+            r.q[0] = a[0];
+            r.q[1] = a[1];
+        }
+    } else {
+        r.q[0] = a[0];
+    }
     return r;
 }
 
@@ -105,8 +120,8 @@ template <int DT> __device__ __forceinline__ void unpack8(const Raw8<DT>& r, flo
     }
 }
 
-template <int DT> __device__ __forceinline__ void store8(void* p, int64_t i, const float (&v)[8]) {
-    uint4* a = reinterpret_cast<uint4*>((char*)p + i * DT_BYTES<DT>);
+template <int DT> __device__ __forceinline__ void store8(char* p, const float (&v)[8], bool wide) {
+    uint4* a = reinterpret_cast<uint4*>(p);
     Raw8<DT> r;
     uint32_t* w = reinterpret_cast<uint32_t*>(&r);
     if constexpr (DT == SOLO_DT_F32) {
@@ -125,8 +140,17 @@ template <int DT> __device__ __forceinline__ void store8(void* p, int64_t i, con
             w[k] = *reinterpret_cast<const uint32_t*>(&b);
         }
     }
-#pragma unroll
-    for (int k = 0; k < DT_BYTES<DT> / 2; ++k) a[k] = r.q[k];
+    if constexpr (DT == SOLO_DT_F32) {
+        if (wide) {
+            asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" :: "l"(a), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                         : "memory");
+        } else {
+            a[0] = r.q[0];
+            a[1] = r.q[1];
+        }
+    } else {
+        a[0] = r.q[0];
+    }
 }
 
 // ---- sums ---------------------------------------------------------------------------------------------------------
@@ -139,38 +163,35 @@ __device__ __forceinline__ double join(int nt, double a, double b) { return nt =
 template <int NT> struct Sum {
     double s = 0.0;
     uint32_t m = 0;
-    template <int N> __device__ __forceinline__ void add(const float (&v)[N]) {
-        if constexpr (NT == SOLO_NORM_MAX) {
+    float c[2] = {0.0f, 0.0f};   // powers of up to 32 values
+    __device__ __forceinline__ void add(const float (&v)[8]) {
 #pragma unroll
-            for (int k = 0; k < N; ++k) m = max(m, __float_as_uint(v[k]) & 0x7FFFFFFFu);
-        } else if constexpr (NT == SOLO_NORM_1) {
-            float c[2] = {0.0f, 0.0f};
+        for (int k = 0; k < 8; ++k) {
+            if constexpr (NT == SOLO_NORM_MAX) m = max(m, __float_as_uint(v[k]) & 0x7FFFFFFFu);
+            else if constexpr (NT == SOLO_NORM_1) c[k & 1] = c[k & 1] + fabsf(v[k]);
+            else c[k & 1] = __fmaf_rn(v[k], v[k], c[k & 1]);
+        }
+    }
+    // Into the binary64 sum; again(u, v) gives the u-th eight of the values added since the last call.
+    template <int N, class Again> __device__ __forceinline__ void settle(Again again) {
+        if constexpr (NT == SOLO_NORM_MAX) return;
+        const float f = c[0] + c[1];
+        c[0] = c[1] = 0.0f;
+        // Above 2^-100, what 32 squares lost below 2^-149 is less than 2^-44 of the sum.
+        if (f < __int_as_float(0x7F800000) && (NT == SOLO_NORM_1 || f >= 0x1p-100f)) {
+            s += (double)f;
+            return;
+        }
+#pragma unroll 1
+        for (int u = 0; u < N; ++u) {
+            float v[8];
+            again(u, v);
+            uint32_t any = 0;
 #pragma unroll
-            for (int k = 0; k < N; ++k) c[k & 1] = c[k & 1] + fabsf(v[k]);
-            const float f = c[0] + c[1];
-            if (f < __int_as_float(0x7F800000)) {
-                s += (double)f;
-            } else {
+            for (int k = 0; k < 8; ++k) any |= __float_as_uint(v[k]);
+            if ((any & 0x7FFFFFFFu) == 0) continue;
 #pragma unroll
-                for (int k = 0; k < N; ++k) s += (double)fabsf(v[k]);
-            }
-        } else if constexpr (NT == SOLO_NORM_2) {
-            float c[2] = {0.0f, 0.0f};
-#pragma unroll
-            for (int k = 0; k < N; ++k) c[k & 1] = __fmaf_rn(v[k], v[k], c[k & 1]);
-            const float f = c[0] + c[1];
-            // Above 2^-100, what N <= 32 squares lost below 2^-149 is less than 2^-44 of the sum.
-            if (f >= 0x1p-100f && f < __int_as_float(0x7F800000)) {
-                s += (double)f;
-            } else {
-                uint32_t any = 0;
-#pragma unroll
-                for (int k = 0; k < N; ++k) any |= __float_as_uint(v[k]);
-                if (any & 0x7FFFFFFFu) {
-#pragma unroll
-                    for (int k = 0; k < N; ++k) s = __fma_rn((double)v[k], (double)v[k], s);
-                }
-            }
+            for (int k = 0; k < 8; ++k) s = NT == SOLO_NORM_1 ? s + (double)fabsf(v[k]) : __fma_rn((double)v[k], (double)v[k], s);
         }
     }
     __device__ __forceinline__ double value() const { return NT == SOLO_NORM_MAX ? (double)__uint_as_float(m) : s; }
@@ -225,10 +246,59 @@ __device__ __forceinline__ int find_tensor(const int64_t* tile_start, int num_te
     return lo;
 }
 
+// The tensor that a tile belongs to, and the tile.
+template <int DS, int DD, bool WRITES> struct Place {
+    int t;
+    int64_t t0, t1;              // the tensor's tiles
+    int64_t n;
+    const char* s;
+    char* d;
+    int head;                    // elements before the first place where vectors of both sides are aligned
+    bool vec, wide;
+
+    __device__ __forceinline__ void tensor(const GradArgs& a, int which) {
+        t = which;
+        t0 = a.tile_start[t];
+        t1 = a.tile_start[t + 1];
+        n = a.numel[t];
+        s = (const char*)a.src[t];
+        d = WRITES ? (char*)a.dst[t] : nullptr;
+        const uintptr_t sa = (uintptr_t)s, da = (uintptr_t)d;
+        // eight elements of the narrower type take 16 bytes; eight of fp32 on a 16-byte boundary two accesses
+        constexpr bool BY_DST = WRITES && DT_BYTES<DD> < DT_BYTES<DS>;
+        head = BY_DST ? (int)(8 - (da / DT_BYTES<DD>) % 8) % 8 : (int)(8 - (sa / DT_BYTES<DS>) % 8) % 8;
+        const uintptr_t sh = sa + head * DT_BYTES<DS>, dh = WRITES ? da + head * DT_BYTES<DD> : 0;
+        vec = ((sh | dh) & 15) == 0;
+        wide = (((DS == SOLO_DT_F32 ? sh : 0) | (DD == SOLO_DT_F32 ? dh : 0)) & 31) == 0;
+        if (!vec) head = 0;
+    }
+    __device__ __forceinline__ void start(const GradArgs& a, int64_t x) { tensor(a, find_tensor(a.tile_start, a.num_tensors, x)); }
+    // To tile x, after or before: the tensors next to the present one, 32 at a time.
+    __device__ __forceinline__ void move(const GradArgs& a, int64_t x) {
+        if (x >= t0 && x < t1) return;
+        const int lane = threadIdx.x & 31;
+        int u = t;
+        for (;;) {
+            int steps;
+            if (x >= t1) {
+                const int probe = u + 1 + lane;
+                steps = __popc(__ballot_sync(0xFFFFFFFFu, probe < a.num_tensors && a.tile_start[probe] <= x));
+                u += steps;
+            } else {
+                const int probe = u - lane;
+                steps = __popc(__ballot_sync(0xFFFFFFFFu, probe >= 0 && a.tile_start[probe] > x));
+                u -= steps;
+            }
+            if (steps < 32) break;
+        }
+        tensor(a, u);
+    }
+};
+
 // ---- the kernel -----------------------------------------------------------------------------------------------------
 
 // DS: type read (gradients); DD: type written; NT: norm type or -1.
-template <int OP, int DS, int DD, int NT> __global__ __launch_bounds__(GCTA) void grad_kernel(const __grid_constant__ GradArgs a) {
+template <int OP, int DS, int DD, int NT> __global__ __launch_bounds__(GCTA, OP == OP_ACC || DS == SOLO_DT_F32 ? (OP == OP_NORM ? 4 : 2) : OP == OP_NORM ? 5 : 4) void grad_kernel(const __grid_constant__ GradArgs a) {
     using S = std::integral_constant<int, DS>;
     using D = std::integral_constant<int, DD>;
     constexpr bool WRITES = OP != OP_NORM;
@@ -238,90 +308,103 @@ template <int OP, int DS, int DD, int NT> __global__ __launch_bounds__(GCTA) voi
     pdl_wait();
     pdl_release();
     const int64_t grid = gridDim.x, c = blockIdx.x;
-    const int64_t lo = a.tiles * c / grid, hi = a.tiles * (c + 1) / grid;
+    const bool shares = SUMS && a.slots;
+    int64_t x = shares ? a.tiles * c / grid : c;                       // of the tiles in the order taken
+    const int64_t end = shares ? a.tiles * (c + 1) / grid : a.tiles, step = shares ? 1 : grid;
+    const auto tile = [&](int64_t i) { return a.backwards ? a.tiles - 1 - i : i; };
     float f = a.scale;
-    if constexpr (OP == OP_CLIP) {
-        double norm;
-        f = clip_factor(a, box[turn], &norm);
-        turn ^= 1;
-        if (a.norm_out && c == 0 && threadIdx.x == 0) *a.norm_out = (float)norm;
-    }
+    bool have_f = OP != OP_CLIP;
     Sum<NT> sum;
     double share = 0.0;
-    int t = lo < hi ? find_tensor(a.tile_start, a.num_tensors, lo) : 0;
-    for (int64_t x = lo; x < hi;) {
-        while (a.tile_start[t + 1] <= x) ++t;                       // past empty tensors
-        const int64_t t0 = a.tile_start[t];
-        const int64_t xe = min(hi, a.tile_start[t + 1]);
-        const int64_t n = a.numel[t];
-        const void* const s = a.src[t];
-        void* const d = WRITES ? a.dst[t] : nullptr;
-        // Elements before the first place where vectors of both sides start on a 16-byte boundary; none: element by element.
-        int head = 0;
-        bool vec;
-        {
-            const uintptr_t sa = (uintptr_t)s, da = (uintptr_t)d;
-            constexpr int narrow = WRITES && DT_BYTES<DD> < DT_BYTES<DS>;
-            if (narrow) head = (int)((16 - (da & 15)) & 15) / DT_BYTES<DD>;
-            else head = (int)((16 - (sa & 15)) & 15) / DT_BYTES<DS>;
-            vec = ((sa + head * DT_BYTES<DS>) & 15) == 0 && (!WRITES || ((da + head * DT_BYTES<DD>) & 15) == 0);
-            if (!vec) head = 0;
-        }
-        if (OP == OP_CLIP && DS == DD && f == 1.0f && s == d) x = xe;       // in place, by one: nothing changes
-        for (; x < xe; ++x) {
-            const int64_t base = head + (x - t0) * GTILE;
-            int64_t e0 = x == t0 ? 0 : base, e1 = min(n, base + GTILE);
-            if (vec && base + GTILE <= n) {
-                Raw8<DS> g[GU];
-                [[maybe_unused]] Raw8<SOLO_DT_F32> acc[OP == OP_ACC ? GU : 1];
+    Place<DS, DD, WRITES> at;
+    if (x < end) at.start(a, tile(x));
+    while (x < end) {
+        const int64_t off = tile(x) - at.t0, base = at.head + off * GTILE;
+        const bool full = at.vec && base + GTILE <= at.n;
+        const int64_t first = off == 0 ? 0 : base;
+        const int rest = (int)(full ? base - first : max(min(at.n, base + GTILE) - first, (int64_t)0));   // elements taken one by one
+        const char* const s = at.s + first * DT_BYTES<DS>;
+        char* const d = at.d + first * DT_BYTES<DD>;
+        const char* const sv = at.s + (base + (int)threadIdx.x * GV) * DT_BYTES<DS>;
+        char* const dv = at.d + (base + (int)threadIdx.x * GV) * DT_BYTES<DD>;
+        const bool wide = at.wide, same = WRITES && (const char*)at.d == at.s;
+        const int t = at.t;
+        Raw8<DS> g[GU];
+        [[maybe_unused]] Raw8<SOLO_DT_F32> acc[OP == OP_ACC ? GU : 1];
+        if (full) {
 #pragma unroll
-                for (int u = 0; u < GU; ++u) {
-                    const int64_t i = base + (u * GCTA + (int)threadIdx.x) * GV;
-                    g[u] = load8<DS>(s, i);
-                    if constexpr (OP == OP_ACC) acc[u] = load8<SOLO_DT_F32>(d, i);
-                }
-                float v[GU * GV];
-#pragma unroll
-                for (int u = 0; u < GU; ++u) {
-                    float w[GV];
-                    unpack8<DS>(g[u], w);
-                    if constexpr (OP == OP_ACC) {
-                        float b[GV];
-                        unpack8<SOLO_DT_F32>(acc[u], b);
-#pragma unroll
-                        for (int k = 0; k < GV; ++k) w[k] = __fmaf_rn(f, w[k], b[k]);
-                    } else if constexpr (WRITES) {
-#pragma unroll
-                        for (int k = 0; k < GV; ++k) w[k] = f * w[k];
-                    }
-                    if constexpr (WRITES) store8<DD>(d, base + (u * GCTA + (int)threadIdx.x) * GV, w);
-#pragma unroll
-                    for (int k = 0; k < GV; ++k) v[u * GV + k] = w[k];
-                }
-                if constexpr (SUMS) sum.add(v);
-                e1 = base;                                          // what is left: the elements before the first vector
+            for (int u = 0; u < GU; ++u) {
+                g[u] = load8<DS>(sv + u * GCTA * GV * DT_BYTES<DS>, wide);
+                if constexpr (OP == OP_ACC) acc[u] = load8<SOLO_DT_F32>(dv + u * GCTA * GV * 4, wide);
             }
-            for (int64_t i0 = e0; i0 < e1; i0 += GCTA * 8) {
-                float w[8];
+        }
+        if constexpr (OP == OP_CLIP) {
+            if (!have_f) {
+                double norm;
+                f = clip_factor(a, box[0], &norm);
+                have_f = true;
+                if (a.norm_out && c == 0 && threadIdx.x == 0) *a.norm_out = (float)norm;
+            }
+        }
+        // (a pass that only reads has other CTAs' loads under way meanwhile, and no registers to spare for a second place)
+        if constexpr (WRITES) {
+            x += step;
+            if (x < end) at.move(a, tile(x));
+        }
+        if (OP == OP_CLIP && DS == DD && f == 1.0f && same) continue;           // in place, by one: nothing changes
+        if (full) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const int64_t i = i0 + k * GCTA + threadIdx.x;
-                    w[k] = i < e1 ? elem_load(s, i, S{}) : 0.0f;
-                    if constexpr (OP == OP_ACC) w[k] = i < e1 ? __fmaf_rn(f, w[k], elem_load(d, i, D{})) : 0.0f;
-                    else if constexpr (WRITES) w[k] = f * w[k];
-                }
-                if constexpr (WRITES) {
+            for (int u = 0; u < GU; ++u) {
+                float w[GV];
+                unpack8<DS>(g[u], w);
+                if constexpr (OP == OP_ACC) {
+                    float b[GV];
+                    unpack8<SOLO_DT_F32>(acc[u], b);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const int64_t i = i0 + k * GCTA + threadIdx.x;
-                        if (i < e1) elem_store(d, i, w[k], D{});
-                    }
+                    for (int k = 0; k < GV; ++k) w[k] = __fmaf_rn(f, w[k], b[k]);
+                } else if constexpr (WRITES) {
+#pragma unroll
+                    for (int k = 0; k < GV; ++k) w[k] = f * w[k];
                 }
+                if constexpr (WRITES) store8<DD>(dv + u * GCTA * GV * DT_BYTES<DD>, w, wide);
                 if constexpr (SUMS) sum.add(w);
             }
+            if constexpr (SUMS)
+                sum.template settle<GU>([&](int u, float (&w)[GV]) {             // from memory again: what was read, or written
+                    if constexpr (WRITES) unpack8<DD>(load8<DD>(dv + u * GCTA * GV * DT_BYTES<DD>, wide), w);
+                    else unpack8<DS>(load8<DS>(sv + u * GCTA * GV * DT_BYTES<DS>, wide), w);
+                });
+        }
+        for (int i0 = threadIdx.x; i0 < rest; i0 += GCTA * 8) {
+            float w[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int i = i0 + k * GCTA;
+                w[k] = i < rest ? elem_load(s, i, S{}) : 0.0f;
+                if constexpr (OP == OP_ACC) w[k] = i < rest ? __fmaf_rn(f, w[k], elem_load(d, i, D{})) : 0.0f;
+                else if constexpr (WRITES) w[k] = f * w[k];
+            }
+            if constexpr (WRITES) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const int i = i0 + k * GCTA;
+                    if (i < rest) elem_store(d, i, w[k], D{});
+                }
+            }
+            if constexpr (SUMS) {
+                sum.add(w);
+                sum.template settle<1>([&](int, float (&v)[8]) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) v[k] = w[k];
+                });
+            }
+        }
+        if constexpr (!WRITES) {
+            x += step;
+            if (x < end) at.move(a, tile(x));
         }
         if constexpr (SUMS) {
-            if (a.slots) {
+            if (shares && (x >= end || at.t != t)) {
                 const double r = cta_join(NT, sum.value(), box[turn]);
                 turn ^= 1;
                 if (threadIdx.x == 0) a.slots[c + t] = r;
@@ -331,8 +414,15 @@ template <int OP, int DS, int DD, int NT> __global__ __launch_bounds__(GCTA) voi
         }
     }
     if constexpr (SUMS) {
-        if (!a.slots) share = cta_join(NT, sum.value(), box[turn]);
+        if (!shares) share = cta_join(NT, sum.value(), box[turn]);
         if (threadIdx.x == 0) a.cta_sum[c] = share;
+    }
+    if constexpr (OP == OP_CLIP) {
+        if (!have_f && a.norm_out) {                                            // a list without elements
+            double norm;
+            clip_factor(a, box[0], &norm);
+            if (threadIdx.x == 0) *a.norm_out = (float)norm;
+        }
     }
 }
 
@@ -501,7 +591,15 @@ int pass(int op, const solo_grad_list_t* src, const solo_grad_list_t* dst, int n
     a.tile_start = g->geom + g->num_tensors;
     a.tiles = g->tiles;
     a.num_tensors = g->num_tensors;
-    const int64_t grid = std::max<int64_t>(1, std::min<int64_t>(g->tiles, (int64_t)sm_count(g->device) * per_sm));
+    // Passes that write run best with no more reads under way than it takes (us with 2, 3, 4, 5, 6 CTAs per SM: accumulation of
+    // 809M bf16 1235, 1288, 1287, 1290, 1300; clip of 125M bf16 in place 92, 81, 79, 93, 94; of 809M fp32 to bf16 768, 786,
+    // 784, 761, 761); a pass that only reads takes all that fit (1903 us for 7B bf16 with 4, 1813 with 5).
+    int most = per_sm;
+    if (op != OP_NORM) {
+        const int per_elem = (src->dtype == SOLO_DT_F32 ? 4 : 2) + (op == OP_ACC ? 4 : 0);
+        most = std::min(per_sm, std::max(2, GIN_FLIGHT / (GTILE * per_elem)));
+    }
+    const int64_t grid = std::max<int64_t>(1, std::min<int64_t>(g->tiles, (int64_t)sm_count(g->device) * most));
     if (grid_out) *grid_out = (int)grid;
     void* params[] = {&a};
     return launch((const void*)k, (unsigned)grid, params, stream);
@@ -639,6 +737,7 @@ int solo_grad_clip_norm(const solo_grad_list_t* src, const solo_grad_list_t* dst
     a.max_norm = max_norm;
     a.scale = scale;
     a.norm_out = norm_dev;
+    a.backwards = 1;             // what the first pass read last is still in L2
     return pass(OP_CLIP, src, dst, -1, a, (cudaStream_t)stream);
 }
 
