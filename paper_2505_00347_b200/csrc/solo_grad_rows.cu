@@ -1,6 +1,6 @@
 // The gradient of an embedding, added to its fp32 accumulator: acc[tok_i, :] += s * g[i, :] (include/solo.h).
 //
-// Two launches for up to 65,536 tokens.  A cluster of up to eight CTAs sorts the tokens with their positions in its shared memory
+// Two launches for up to 65,536 tokens.  A cluster of up to sixteen CTAs sorts the tokens with their positions in its shared memory
 // (least significant digit first, stable, so that equal tokens keep their order); then a CTA takes 128 entries of the sorted
 // order and 256 columns, a warp 16 of these entries.  A warp sums the rows of each run of equal tokens in registers; runs that
 // lie in one warp's entries are added to the accumulator at once, the pieces of others are put together in shared memory, and those of
@@ -29,14 +29,13 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int SORT_CTA = 1024;
+constexpr int SORT_CTA = 256;
 constexpr int SORT_WARPS = SORT_CTA / 32;
-constexpr int SORT_CLUSTER = 8;                        // most CTAs of the sort
-constexpr int SORT_PER_CTA = 8192;                     // most tokens of one of them
-constexpr int SORT_ROUNDS = SORT_PER_CTA / SORT_CTA;   // tokens per thread
-constexpr int SORT_SMALL = 2048;                       // tokens per CTA that the cluster's size aims at
+constexpr int SORT_CLUSTER = 16;                       // most CTAs of the sort
+constexpr int SORT_PER_CTA = 4096;                     // most tokens of one of them
+constexpr int SORT_AIM = 1024;                         // tokens per CTA that the cluster's size aims at
 constexpr int CHUNK = SORT_CLUSTER * SORT_PER_CTA;     // tokens per pair of launches
-constexpr int DIGIT_MIN = 5, DIGIT_MAX = 9, DIGITS = 1 << DIGIT_MAX;
+constexpr int DIGIT_MAX = 9, DIGITS = 1 << DIGIT_MAX;
 
 constexpr int ROWS_WARPS = 8, ROWS_CTA = ROWS_WARPS * 32;   // of the summing kernel
 constexpr int WARP_ROWS = 16, CTA_ROWS = ROWS_WARPS * WARP_ROWS;
@@ -55,15 +54,16 @@ struct SortArgs {
 
 struct SortShared {
     uint2 item[2][SORT_PER_CTA];                // token, position
-    uint16_t hist[SORT_WARPS * DIGITS];         // [warp][digit] of each warp, then how many of a digit lie in the warps before
-    uint32_t part[SORT_CTA];                    // [group of warps][digit]: how many
-    uint32_t before[SORT_CTA];                  // the same: how many in the groups before
+    uint16_t hist[SORT_WARPS][DIGITS];          // of each warp, then how many of a digit lie in the warps before
     uint32_t total[SORT_CLUSTER][DIGITS];       // of each CTA
     uint32_t base[DIGITS];                      // first place of a digit's tokens of this CTA
     uint32_t scan[SORT_WARPS];
 };
 
-__global__ __launch_bounds__(SORT_CTA) void rows_sort_kernel(const __grid_constant__ SortArgs a) {
+// The time goes into latencies (16,384 tokens, two passes: 1024 threads in eight CTAs 12.5 us, 256 threads in sixteen @@ us).
+// ROUNDS: tokens per thread, at most; BITS: of a digit, at most.
+template <int ROUNDS, int BITS> __global__ __launch_bounds__(SORT_CTA) void rows_sort_kernel(const __grid_constant__ SortArgs a) {
+    constexpr uint32_t ALL = 0xFFFFFFFFu, NONE = 0xFFFFFFFFu;
     extern __shared__ __align__(16) unsigned char smem[];
     SortShared& s = *reinterpret_cast<SortShared*>(smem);
     cg::cluster_group cluster = cg::this_cluster();
@@ -75,104 +75,122 @@ __global__ __launch_bounds__(SORT_CTA) void rows_sort_kernel(const __grid_consta
     const int per_cta = 1 << a.log_per_cta;
     const int first = me * per_cta;
     const int count = min(max(a.num_tokens - first, 0), per_cta);
-    for (int j = tid; j < count; j += SORT_CTA) {
-        const int64_t t = a.token_bytes == 8 ? ((const int64_t*)a.tokens)[first + j] : (int64_t)((const int32_t*)a.tokens)[first + j];
-        s.item[0][j] = make_uint2(t >= 0 && t < a.num_rows ? (uint32_t)t : (uint32_t)a.num_rows, (uint32_t)(first + j));
+    const int rounds = (per_cta + SORT_CTA - 1) / SORT_CTA;
+    const uint32_t digits = 1u << a.digit_bits;
+    // A warp's tokens follow one another; first from global memory, then from this CTA's places.
+    uint2 item[ROUNDS];
+    uint32_t rank[ROUNDS];
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+        const int j = (warp * rounds + r) * 32 + lane;
+        if (r < rounds && j < count) {
+            const int64_t t = a.token_bytes == 8 ? ((const int64_t*)a.tokens)[first + j] : (int64_t)((const int32_t*)a.tokens)[first + j];
+            item[r] = make_uint2(t >= 0 && t < a.num_rows ? (uint32_t)t : (uint32_t)a.num_rows, (uint32_t)(first + j));
+        }
     }
     for (int i = me * SORT_CTA + tid; i < a.num_counters; i += ctas * SORT_CTA) a.counters[i] = 0;
-    const int digits = 1 << a.digit_bits;
-    const int rounds = (per_cta + SORT_CTA - 1) / SORT_CTA;
-    uint16_t* const hist = s.hist + warp * digits;
-    // for the sums over warps: threads of a group of warps (one for each digit), and the warps of a group
-    const int group = tid >> a.digit_bits, digit = tid & (digits - 1), group_warps = digits / 32;
     cluster.barrier_wait();
     for (int p = 0; p < a.passes; ++p) {
-        const int shift = p * a.digit_bits, from = p & 1;
-        for (int i = lane; i < digits / 2; i += 32) reinterpret_cast<uint32_t*>(hist)[i] = 0;
-        __syncthreads();                        // (the tokens)
-        // Place of every token among those of its digit in its warp.
-        uint2 item[SORT_ROUNDS];
-        uint32_t rank[SORT_ROUNDS];
+        const int shift = p * a.digit_bits, to_buf = p & 1;
+        for (uint32_t i = lane; i < digits / 2; i += 32) reinterpret_cast<uint32_t*>(s.hist[warp])[i] = 0;
+        if (digits < 2 && lane == 0) s.hist[warp][0] = 0;
+        __syncwarp();
+        // Place of every token among those of its digit in its warp.  Lanes with the same digit: a vote for each of its bits (a
+        // match over the warp takes a step for each distinct digit).
 #pragma unroll
-        for (int r = 0; r < SORT_ROUNDS; ++r) {
+        for (int r = 0; r < ROUNDS; ++r) {
             if (r < rounds) {
-                const int j = (warp * rounds + r) * 32 + lane;
-                const bool have = j < count;
-                item[r] = have ? s.item[from][j] : make_uint2(0, 0);
-                const int d = have ? (int)((item[r].x >> shift) & (uint32_t)(digits - 1)) : digits;
-                // Lanes with the same digit, a vote for each of its bits (a match over the warp takes a step per distinct
-                // digit: 2000 cycles a round where this takes 300).
-                uint32_t peers = __ballot_sync(0xFFFFFFFFu, have);
+                const bool have = (warp * rounds + r) * 32 + lane < count;
+                const uint32_t d = (item[r].x >> shift) & (digits - 1);
+                uint32_t peers = __ballot_sync(ALL, have);
 #pragma unroll
-                for (int b = 0; b < DIGIT_MAX; ++b) {
+                for (int b = 0; b < BITS; ++b) {
                     const bool bit = (d >> b) & 1;
-                    const uint32_t vote = __ballot_sync(0xFFFFFFFFu, bit);
+                    const uint32_t vote = __ballot_sync(ALL, bit);
                     peers &= bit ? vote : ~vote;
                 }
-                const uint32_t before = peers & ((1u << lane) - 1u);
-                rank[r] = have ? hist[d] + __popc(before) : 0xFFFFFFFFu;
-                __syncwarp();
-                if (have && before == 0) hist[d] = (uint16_t)(hist[d] + __popc(peers));
-                __syncwarp();
+                rank[r] = have ? peers : 0;
             }
-        }
-        __syncthreads();
-        uint32_t sum = 0;
-#pragma unroll 8
-        for (int w = group * group_warps; w < (group + 1) * group_warps; ++w) {
-            const uint32_t h = s.hist[w * digits + digit];
-            s.hist[w * digits + digit] = (uint16_t)sum;
-            sum += h;
-        }
-        s.part[tid] = sum;
-        __syncthreads();
-        uint32_t before_group = 0, total = 0;
-        for (int g = 0; g < SORT_CTA >> a.digit_bits; ++g) {
-            const uint32_t v = s.part[(g << a.digit_bits) + digit];
-            if (g < group) before_group += v;
-            total += v;
-        }
-        s.before[tid] = before_group;
-        if (group == 0)
-            for (int r = 0; r < ctas; ++r) cluster.map_shared_rank(&s, r)->total[me][digit] = total;
-        cluster.sync();
-        // Digits before this one in the whole cluster, then the CTAs before this one.
-        uint32_t all = 0, mine = 0, upto = 0;
-        if (tid < digits) {
-            for (int r = 0; r < ctas; ++r) {
-                if (r == me) mine = all;
-                all += s.total[r][tid];
-            }
-            upto = all;
         }
 #pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) {
+            if (r < rounds) {
+                const uint32_t peers = rank[r], before = peers & ((1u << lane) - 1u);
+                uint16_t* const h = &s.hist[warp][(item[r].x >> shift) & (digits - 1)];
+                const uint32_t seen = peers ? *h : 0;
+                __syncwarp();
+                if (peers && before == 0) *h = (uint16_t)(seen + __popc(peers));
+                __syncwarp();
+                rank[r] = peers ? seen + __popc(before) : NONE;
+            }
+        }
+        __syncthreads();
+        // Over the warps, then over the CTAs; a thread has one or two digits, next to each other.
+        const int own = digits > SORT_CTA ? 2 : 1;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const uint32_t d = tid * own + k;
+            if (k < own && d < digits) {
+                uint32_t h[SORT_WARPS], sum = 0;
+#pragma unroll
+                for (int w = 0; w < SORT_WARPS; ++w) h[w] = s.hist[w][d];
+#pragma unroll
+                for (int w = 0; w < SORT_WARPS; ++w) {
+                    s.hist[w][d] = (uint16_t)sum;
+                    sum += h[w];
+                }
+                for (int r = 0; r < ctas; ++r) cluster.map_shared_rank(&s, r)->total[me][d] = sum;
+            }
+        }
+        cluster.sync();
+        uint32_t all[2] = {0, 0}, mine[2] = {0, 0};
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const uint32_t d = tid * own + k;
+            if (k < own && d < digits)
+                for (int r = 0; r < ctas; ++r) {
+                    if (r == me) mine[k] = all[k];
+                    all[k] += s.total[r][d];
+                }
+        }
+        uint32_t upto = all[0] + all[1];
+#pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
-            const uint32_t o = __shfl_up_sync(0xFFFFFFFFu, upto, d);
+            const uint32_t o = __shfl_up_sync(ALL, upto, d);
             if (lane >= d) upto += o;
         }
         if (lane == 31) s.scan[warp] = upto;
         __syncthreads();
-        if (tid < digits) {
-            uint32_t b = upto - all + mine;
-            for (int w = 0; w < warp; ++w) b += s.scan[w];
-            s.base[tid] = b;
+        uint32_t start = upto - all[0] - all[1];
+#pragma unroll
+        for (int w = 0; w < SORT_WARPS; ++w) start += w < warp ? s.scan[w] : 0;
+        if ((uint32_t)(tid * own) < digits) {
+            s.base[tid * own] = start + mine[0];
+            if (own == 2) s.base[tid * 2 + 1] = start + all[0] + mine[1];
         }
         __syncthreads();
 #pragma unroll
-        for (int r = 0; r < SORT_ROUNDS; ++r) {
-            if (r < rounds && rank[r] != 0xFFFFFFFFu) {
-                const int d = (int)((item[r].x >> shift) & (uint32_t)(digits - 1));
-                const uint32_t to = s.base[d] + s.before[(warp / group_warps << a.digit_bits) + d] + hist[d] + rank[r];
-                cluster.map_shared_rank(&s, to >> a.log_per_cta)->item[from ^ 1][to & (uint32_t)(per_cta - 1)] = item[r];
+        for (int r = 0; r < ROUNDS; ++r) {
+            if (r < rounds && rank[r] != NONE) {
+                const uint32_t d = (item[r].x >> shift) & (digits - 1);
+                const uint32_t to = s.base[d] + s.hist[warp][d] + rank[r];
+                cluster.map_shared_rank(&s, to >> a.log_per_cta)->item[to_buf][to & (uint32_t)(per_cta - 1)] = item[r];
             }
         }
         cluster.sync();
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) {
+            const int j = (warp * rounds + r) * 32 + lane;
+            if (r < rounds && j < count) item[r] = s.item[to_buf][j];
+        }
     }
-    const int last = a.passes & 1;
-    for (int j = tid; j < count; j += SORT_CTA) {
-        const uint2 v = s.item[last][j];
-        a.tok[first + j] = v.x;
-        a.pos[first + j] = (uint16_t)v.y;
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+        const int j = (warp * rounds + r) * 32 + lane;
+        if (r < rounds && j < count) {
+            a.tok[first + j] = item[r].x;
+            a.pos[first + j] = (uint16_t)item[r].y;
+        }
     }
 }
 
@@ -547,19 +565,28 @@ int launch(const void* k, dim3 grid, unsigned threads, size_t smem, int cluster,
     return SOLO_OK;
 }
 
-// The sort's shared memory, opted in to once per device.
+using SortKernel = void (*)(const SortArgs);
+SortKernel sort_kernel_for(int rounds, int bits) {
+    if (rounds <= 4) return bits <= 8 ? rows_sort_kernel<4, 8> : rows_sort_kernel<4, DIGIT_MAX>;
+    return bits <= 8 ? rows_sort_kernel<SORT_PER_CTA / SORT_CTA, 8> : rows_sort_kernel<SORT_PER_CTA / SORT_CTA, DIGIT_MAX>;
+}
+
+// The sort's shared memory and clusters of sixteen, opted in to once per device.
 int sort_ready() {
     static std::atomic<bool> done[64];
     int device = -1;
     if (cudaGetDevice(&device) != cudaSuccess || device < 0 || device >= 64) { cudaGetLastError(); return SOLO_ECUDA; }
-    if (!done[device]) {
-        if (cudaFuncSetAttribute((const void*)rows_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SortShared)) !=
-            cudaSuccess) {
-            cudaGetLastError();
-            return SOLO_ECUDA;
+    if (done[device]) return SOLO_OK;
+    for (int rounds : {4, 16})
+        for (int bits : {8, DIGIT_MAX}) {
+            const void* k = (const void*)sort_kernel_for(rounds, bits);
+            if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SortShared)) != cudaSuccess ||
+                cudaFuncSetAttribute(k, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
+                cudaGetLastError();
+                return SOLO_ECUDA;
+            }
         }
-        done[device] = true;
-    }
+    done[device] = true;
     return SOLO_OK;
 }
 
@@ -644,16 +671,16 @@ int solo_grad_accumulate_rows(const solo_grad_rows_t* r, float scale, void* work
         s.num_tokens = n;
         s.num_rows = (int32_t)r->num_rows;
         s.passes = (bits + DIGIT_MAX - 1) / DIGIT_MAX;
-        s.digit_bits = std::max(DIGIT_MIN, (bits + s.passes - 1) / s.passes);
+        s.digit_bits = (bits + s.passes - 1) / s.passes;
         s.tok = (uint32_t*)(ws + l.tok);
         s.pos = (uint16_t*)(ws + l.pos);
         s.counters = (uint32_t*)(ws + l.counters);
         s.num_counters = (int32_t)row_ctas;
         int ctas = 1;
-        while (ctas < SORT_CLUSTER && n > ctas * SORT_SMALL) ctas *= 2;
+        while (ctas < SORT_CLUSTER && n > ctas * SORT_AIM) ctas *= 2;
         while ((ctas << s.log_per_cta) < n) ++s.log_per_cta;
         void* sp[] = {&s};
-        rc = launch((const void*)rows_sort_kernel, dim3((unsigned)ctas), SORT_CTA, sizeof(SortShared), ctas, sp, stream);
+        rc = launch((const void*)sort_kernel_for((1 << s.log_per_cta) / SORT_CTA, s.digit_bits), dim3((unsigned)ctas), SORT_CTA, sizeof(SortShared), ctas, sp, stream);
         if (rc != SOLO_OK) return rc;
         RowsArgs a;
         std::memset(&a, 0, sizeof(a));
