@@ -39,7 +39,7 @@ constexpr int DIGIT_MAX = 9, DIGITS = 1 << DIGIT_MAX;
 
 constexpr int ROWS_WARPS = 8, ROWS_CTA = ROWS_WARPS * 32;   // of the summing kernel
 constexpr int WARP_ROWS = 16, CTA_ROWS = ROWS_WARPS * WARP_ROWS;
-constexpr int SLAB = 256;                              // columns of a CTA
+constexpr int RV = 8, SLAB = 32 * RV;                  // columns of a lane; of a CTA
 
 struct SortArgs {
     const void* tokens;
@@ -212,35 +212,40 @@ template <int DT> __device__ __forceinline__ float row_elem(const void* g, int64
     else return __half2float(((const __half*)g)[i]);
 }
 
-// Eight columns of a thread: consecutive ones and 16-byte accesses (VEC), or one in every 32.
+// RV columns of a thread: consecutive ones and wide accesses (VEC), or one in every 32.
 template <int DT, bool VEC> struct Cols {
+    static constexpr int WORDS = VEC && DT != SOLO_DT_F32 ? RV / 2 : RV;
     int64_t c0, width;
     __device__ __forceinline__ int64_t at(int k) const { return VEC ? c0 + k : c0 + k * 32; }
     __device__ __forceinline__ bool in(int k) const { return VEC ? c0 < width : at(k) < width; }
-    struct Raw { uint32_t w[VEC && DT != SOLO_DT_F32 ? 4 : 8]; };
+    struct Raw { uint32_t w[WORDS]; };
     __device__ __forceinline__ Raw load(const void* g, int64_t row) const {
         Raw r;
         if constexpr (VEC) {
-            constexpr int Q = DT == SOLO_DT_F32 ? 2 : 1;
-            const uint4* p = reinterpret_cast<const uint4*>((const char*)g + (row + c0) * (DT == SOLO_DT_F32 ? 4 : 2));
+            const char* const p = (const char*)g + (row + c0) * (DT == SOLO_DT_F32 ? 4 : 2);
+            if constexpr (WORDS % 4 == 0) {
 #pragma unroll
-            for (int q = 0; q < Q; ++q) {
-                const uint4 v = c0 < width ? p[q] : make_uint4(0, 0, 0, 0);
-                r.w[4 * q] = v.x; r.w[4 * q + 1] = v.y; r.w[4 * q + 2] = v.z; r.w[4 * q + 3] = v.w;
+                for (int q = 0; q < WORDS / 4; ++q) {
+                    const uint4 v = c0 < width ? __ldcs(reinterpret_cast<const uint4*>(p) + q) : make_uint4(0, 0, 0, 0);    // read once
+                    r.w[4 * q] = v.x; r.w[4 * q + 1] = v.y; r.w[4 * q + 2] = v.z; r.w[4 * q + 3] = v.w;
+                }
+            } else {
+                const uint2 v = c0 < width ? __ldcs(reinterpret_cast<const uint2*>(p)) : make_uint2(0, 0);
+                r.w[0] = v.x; r.w[1] = v.y;
             }
         } else {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) r.w[k] = in(k) ? __float_as_uint(row_elem<DT>(g, row + at(k))) : 0u;
+            for (int k = 0; k < RV; ++k) r.w[k] = in(k) ? __float_as_uint(row_elem<DT>(g, row + at(k))) : 0u;
         }
         return r;
     }
-    __device__ __forceinline__ static void add(const Raw& r, float (&s)[8]) {
+    __device__ __forceinline__ static void add(const Raw& r, float (&s)[RV]) {
         if constexpr (!VEC || DT == SOLO_DT_F32) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) s[k] += __uint_as_float(r.w[k]);
+            for (int k = 0; k < RV; ++k) s[k] += __uint_as_float(r.w[k]);
         } else {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < RV / 2; ++k) {
                 if constexpr (DT == SOLO_DT_BF16) {
                     s[2 * k] += __uint_as_float(r.w[k] << 16);
                     s[2 * k + 1] += __uint_as_float(r.w[k] & 0xFFFF0000u);
@@ -252,65 +257,62 @@ template <int DT, bool VEC> struct Cols {
             }
         }
     }
-    __device__ __forceinline__ void load_f32(const float* p, float (&v)[8]) const {
+    __device__ __forceinline__ void load_f32(const float* p, float (&v)[RV]) const {
         if constexpr (VEC) {
             if (c0 < width) {
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
+                for (int q = 0; q < RV / 4; ++q) {
                     const float4 f = __ldcg(reinterpret_cast<const float4*>(p + c0) + q);
                     v[4 * q] = f.x; v[4 * q + 1] = f.y; v[4 * q + 2] = f.z; v[4 * q + 3] = f.w;
                 }
             }
         } else {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) if (in(k)) v[k] = __ldcg(p + at(k));
+            for (int k = 0; k < RV; ++k) if (in(k)) v[k] = __ldcg(p + at(k));
         }
     }
-    __device__ __forceinline__ void store_f32(float* p, const float (&v)[8]) const {
+    __device__ __forceinline__ void store_f32(float* p, const float (&v)[RV]) const {
         if constexpr (VEC) {
             if (c0 < width) {
 #pragma unroll
-                for (int q = 0; q < 2; ++q)
+                for (int q = 0; q < RV / 4; ++q)
                     reinterpret_cast<float4*>(p + c0)[q] = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
             }
         } else {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) if (in(k)) p[at(k)] = v[k];
+            for (int k = 0; k < RV; ++k) if (in(k)) p[at(k)] = v[k];
         }
     }
 };
 
-// What the CTAs and warps before and after do is known from the tokens next to their borders.
-__device__ __forceinline__ int ctas_before(const uint32_t* tok, int c, uint32_t t) {       // that a run reaches back into from CTA c
-    int k = 0;
-    for (;;) {
-        const int e = (c - k - (int)(threadIdx.x & 31)) * CTA_ROWS - 1;
-        const uint32_t same = __ballot_sync(0xFFFFFFFFu, e >= 0 && tok[e] == t);
-        if (same != 0xFFFFFFFFu) return k + __ffs(~same) - 1;
-        k += 32;
-    }
+// How many CTAs a run of token t reaches back into from CTA c, or on into: from the tokens next to the CTAs' borders, one
+// border a lane.  The first 32 of them are read by the caller ahead of time.
+__device__ __forceinline__ uint32_t border_before(const uint32_t* tok, int c, int k) {
+    const int e = (c - k - (int)(threadIdx.x & 31)) * CTA_ROWS - 1;
+    return e >= 0 ? tok[e] : 0xFFFFFFFFu;
 }
-__device__ __forceinline__ int ctas_after(const uint32_t* tok, int n, int c, uint32_t t) {  // that it reaches on into
-    int k = 0;
-    for (;;) {
-        const int64_t e = (int64_t)(c + 1 + k + (int)(threadIdx.x & 31)) * CTA_ROWS;
-        const uint32_t same = __ballot_sync(0xFFFFFFFFu, e < n && tok[e] == t);
+__device__ __forceinline__ uint32_t border_after(const uint32_t* tok, int n, int c, int k) {
+    const int e = (c + 1 + k + (int)(threadIdx.x & 31)) * CTA_ROWS;
+    return e < n ? tok[e] : 0xFFFFFFFFu;
+}
+template <class Border> __device__ __forceinline__ int ctas_reached(uint32_t first, uint32_t t, Border border) {
+    for (int k = 0;; k += 32) {
+        const uint32_t same = __ballot_sync(0xFFFFFFFFu, (k ? border(k) : first) == t);
         if (same != 0xFFFFFFFFu) return k + __ffs(~same) - 1;
-        k += 32;
     }
 }
 
 struct SumShared {
     union {
-        float open[2][ROWS_WARPS][8][32];       // pieces of runs that a warp does not hold whole: what continues one, what begins one
-        double join[ROWS_WARPS][8][32];
+        float open[2][ROWS_WARPS][RV][32];       // pieces of runs that a warp does not hold whole: what continues one, what begins one
+        double join[ROWS_WARPS][RV][32];
     };
     uint32_t head[ROWS_WARPS];                  // 0: the warp's first run is its own; 1: continues one and ends here; 2: goes on
     int32_t job[2][2];                          // runs to put together: first CTA (-1: none), CTAs after it
     uint32_t job_tok[2];
 };
 
-template <int DT, bool VEC> __global__ __launch_bounds__(ROWS_CTA) void rows_sum_kernel(const __grid_constant__ RowsArgs a) {
+template <int DT, bool VEC> __global__ __launch_bounds__(ROWS_CTA, 4) void rows_sum_kernel(const __grid_constant__ RowsArgs a) {
     constexpr uint32_t ALL = 0xFFFFFFFFu, NONE = 0xFFFFFFFFu;
     __shared__ SumShared s;
     pdl_wait();
@@ -333,14 +335,18 @@ template <int DT, bool VEC> __global__ __launch_bounds__(ROWS_CTA) void rows_sum
     const bool through = continues && goes_on && ends == 0;             // and these are one
     Cols<DT, VEC> cols;
     cols.width = a.width;
-    cols.c0 = (int64_t)slab * SLAB + (VEC ? lane * 8 : lane);
+    cols.c0 = (int64_t)slab * SLAB + (VEC ? lane * RV : lane);
+    const uint32_t borders_before = warp == 0 && continues ? border_before(a.tok, c, 0) : NONE;
+    const uint32_t borders_after = goes_on ? border_after(a.tok, n, c, 0) : NONE;
     if (threadIdx.x < 2) s.job[threadIdx.x][0] = -1;
     if (lane == 0) s.head[warp] = continues ? (through ? 2 : 1) : 0;
-    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    constexpr int BATCH = 4;
+    float sum[RV] = {};
+    // Entries whose loads are under way together.  Small, for four CTAs per SM: 4 in three CTAs 74.6 us for 16,384 tokens of
+    // 4096 columns, 4 in two 84, 8 in two 80, 2 in four 72.8; four columns per lane gave 72 to 110.
+    constexpr int BATCH = 2;
     for (int k = 0; k < count; k += BATCH) {
         typename Cols<DT, VEC>::Raw r[BATCH];
-        float v[BATCH][8];
+        float v[BATCH][RV];
         float* row[BATCH];
         bool whole[BATCH];                                              // entry that ends a run of this warp alone
 #pragma unroll
@@ -362,15 +368,15 @@ template <int DT, bool VEC> __global__ __launch_bounds__(ROWS_CTA) void rows_sum
                 if ((ends >> x & 1u) || x == count - 1) {
                     if (whole[b]) {
 #pragma unroll
-                        for (int q = 0; q < 8; ++q) v[b][q] = __fmaf_rn(a.scale, sum[q], v[b][q]);
+                        for (int q = 0; q < RV; ++q) v[b][q] = __fmaf_rn(a.scale, sum[q], v[b][q]);
                         cols.store_f32(row[b], v[b]);
                     } else {
                         const int which = continues && (ends & ((1u << x) - 1u)) == 0 ? 0 : 1;
 #pragma unroll
-                        for (int q = 0; q < 8; ++q) s.open[which][warp][q][lane] = sum[q];
+                        for (int q = 0; q < RV; ++q) s.open[which][warp][q][lane] = sum[q];
                     }
 #pragma unroll
-                    for (int q = 0; q < 8; ++q) sum[q] = 0.0f;
+                    for (int q = 0; q < RV; ++q) sum[q] = 0.0f;
                 }
             }
         }
@@ -380,27 +386,27 @@ template <int DT, bool VEC> __global__ __launch_bounds__(ROWS_CTA) void rows_sum
     for (int side = 0; side < 2; ++side) {
         if (side == 0 ? !(warp == 0 && continues) : !(goes_on && !through)) continue;
         bool open = side == 1 || through;
-        float v[8];
+        float v[RV];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] = s.open[side][warp][q][lane];
+        for (int q = 0; q < RV; ++q) v[q] = s.open[side][warp][q][lane];
         for (int u = warp + 1; open && u < ROWS_WARPS; ++u) {
 #pragma unroll
-            for (int q = 0; q < 8; ++q) v[q] += s.open[0][u][q][lane];
+            for (int q = 0; q < RV; ++q) v[q] += s.open[0][u][q][lane];
             open = s.head[u] == 2;
         }
         const uint32_t t = __shfl_sync(ALL, tok, side == 0 ? 0 : WARP_ROWS - 1);
         if (side == 1 && !open) {
             float* const row = a.acc + (int64_t)t * a.width;
-            float old[8];
+            float old[RV];
             cols.load_f32(row, old);
 #pragma unroll
-            for (int q = 0; q < 8; ++q) old[q] = __fmaf_rn(a.scale, v[q], old[q]);
+            for (int q = 0; q < RV; ++q) old[q] = __fmaf_rn(a.scale, v[q], old[q]);
             cols.store_f32(row, old);
             continue;
         }
         cols.store_f32(a.partial + (int64_t)(side == 0 ? c : first_of_second + c) * a.width, v);
-        const int from = side == 0 ? c - ctas_before(a.tok, c, t) : c;
-        const int to = open ? c + ctas_after(a.tok, n, c, t) : c;
+        const int from = side == 0 ? c - ctas_reached(borders_before, t, [&](int k) { return border_before(a.tok, c, k); }) : c;
+        const int to = open ? c + ctas_reached(borders_after, t, [&](int k) { return border_after(a.tok, n, c, k); }) : c;
         __threadfence();
         __syncwarp();
         if (lane == 0 && atomicAdd(&a.counters[(int64_t)from * a.slabs + slab], 1u) == (uint32_t)(to - from)) {
@@ -414,23 +420,23 @@ template <int DT, bool VEC> __global__ __launch_bounds__(ROWS_CTA) void rows_sum
         const int from = s.job[side][0], more = s.job[side][1];
         if (from < 0) continue;
         __threadfence();
-        double d[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        double d[RV] = {};
 #pragma unroll 4
         for (int p = warp; p <= more; p += ROWS_WARPS) {
-            float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+            float v[RV] = {};
             cols.load_f32(a.partial + (int64_t)(p == 0 ? first_of_second + from : from + p) * a.width, v);
 #pragma unroll
-            for (int q = 0; q < 8; ++q) d[q] += (double)v[q];
+            for (int q = 0; q < RV; ++q) d[q] += (double)v[q];
         }
         __syncthreads();                                                // of the other side's sums
 #pragma unroll
-        for (int q = 0; q < 8; ++q) s.join[warp][q][lane] = d[q];
+        for (int q = 0; q < RV; ++q) s.join[warp][q][lane] = d[q];
         __syncthreads();
         double all = 0.0;
 #pragma unroll
-        for (int u = 0; u < ROWS_WARPS; ++u) all += s.join[u][warp][lane];
-        const int64_t col = (int64_t)slab * SLAB + (VEC ? lane * 8 + warp : warp * 32 + lane);
-        if (col < a.width) {
+        for (int u = 0; u < ROWS_WARPS; ++u) all += s.join[u][warp % RV][lane];
+        const int64_t col = (int64_t)slab * SLAB + (VEC ? lane * RV + warp : warp * 32 + lane);
+        if (warp < RV && col < a.width) {
             float* const at = a.acc + (int64_t)s.job_tok[side] * a.width + col;
             *at = __fmaf_rn(a.scale, (float)all, *at);
         }
@@ -452,7 +458,7 @@ struct DirectArgs {
 
 template <int DT, bool VEC> __global__ __launch_bounds__(ROWS_CTA) void rows_direct_kernel(const __grid_constant__ DirectArgs a) {
     constexpr uint32_t ALL = 0xFFFFFFFFu;
-    __shared__ float part[ROWS_WARPS][8][32];
+    __shared__ float part[ROWS_WARPS][RV][32];
     __shared__ uint32_t found[ROWS_WARPS];             // 1: the token is among the warp's, 2: before this CTA's
     pdl_wait();
     pdl_release();
@@ -480,15 +486,15 @@ template <int DT, bool VEC> __global__ __launch_bounds__(ROWS_CTA) void rows_dir
     if (alone && !have) return;
     Cols<DT, VEC> cols;
     cols.width = a.width;
-    cols.c0 = (int64_t)slab * SLAB + (VEC ? lane * 8 : lane);
+    cols.c0 = (int64_t)slab * SLAB + (VEC ? lane * RV : lane);
     float* const row = a.acc + t * a.width;
-    float old[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    float old[RV] = {};
     if (alone) cols.load_f32(row, old);
-    float total[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    float total[RV] = {};
     constexpr int BATCH = 4;
 #pragma unroll
     for (int k = 0; k < DIRECT_WORDS; ++k) {
-        float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        float sum[RV] = {};
         uint32_t left = m[k];
         while (left) {
             typename Cols<DT, VEC>::Raw r[BATCH];
@@ -504,22 +510,22 @@ template <int DT, bool VEC> __global__ __launch_bounds__(ROWS_CTA) void rows_dir
                 if (on[b]) cols.add(r[b], sum);
         }
 #pragma unroll
-        for (int q = 0; q < 8; ++q) total[q] += sum[q];
+        for (int q = 0; q < RV; ++q) total[q] += sum[q];
     }
     if (alone) {
 #pragma unroll
-        for (int q = 0; q < 8; ++q) old[q] = __fmaf_rn(a.scale, total[q], old[q]);
+        for (int q = 0; q < RV; ++q) old[q] = __fmaf_rn(a.scale, total[q], old[q]);
         cols.store_f32(row, old);
         return;
     }
 #pragma unroll
-    for (int q = 0; q < 8; ++q) part[warp][q][lane] = total[q];
+    for (int q = 0; q < RV; ++q) part[warp][q][lane] = total[q];
     __syncthreads();
-    const int64_t col = (int64_t)slab * SLAB + (VEC ? lane * 8 + warp : warp * 32 + lane);
-    if (col < a.width) {
+    const int64_t col = (int64_t)slab * SLAB + (VEC ? lane * RV + warp : warp * 32 + lane);
+    if (warp < RV && col < a.width) {
         float v = 0.0f;
 #pragma unroll
-        for (int u = 0; u < ROWS_WARPS; ++u) v += part[u][warp][lane];
+        for (int u = 0; u < ROWS_WARPS; ++u) v += part[u][warp % RV][lane];
         row[col] = __fmaf_rn(a.scale, v, row[col]);
     }
 }
@@ -638,7 +644,7 @@ int solo_grad_accumulate_rows(const solo_grad_rows_t* r, float scale, void* work
         ((uintptr_t)r->grad & (unsigned)(es - 1)))
         return SOLO_EALIGN;
     cudaStream_t stream = (cudaStream_t)stream_;
-    const bool vec = r->width % 8 == 0 && (((uintptr_t)r->acc | (uintptr_t)r->grad) & 15u) == 0 && (r->grad_stride * es) % 16 == 0;
+    const bool vec = r->width % RV == 0 && (((uintptr_t)r->acc | (uintptr_t)r->grad) & 15u) == 0 && (r->grad_stride * es) % 16 == 0;
     const RowsLayout l = rows_layout(r->num_tokens, r->width);
     if (direct) {
         DirectArgs d;
