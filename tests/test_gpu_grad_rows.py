@@ -83,6 +83,29 @@ def test_widths_and_types(dtype, width):
             check(acc, tokens_of("skewed", n, 400).cuda(), grad, 0.125)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("n,width", [(6000, 4096), (6000, 4099), (20000, 1288), (65536, 300), (130000, 264)])
+def test_more_rows_than_fill_the_gpu_once(dtype, n, width):
+    gen = torch.Generator(device="cuda").manual_seed(width)
+    for kind in ("same", "skewed", "few", "distinct"):
+        acc = torch.randn(3000, width, generator=gen, device="cuda")
+        grad = torch.empty(n, width, device="cuda", dtype=DT[dtype]).normal_(generator=gen)
+        check(acc, tokens_of(kind, n, 3000).cuda(), grad, -1.5)
+
+
+@pytest.mark.parametrize("over", [0, 1, 7, 8, 9, 15, 16, 17, 127, 128, 129, 136, 137, 256, 300])
+def test_runs_over_the_borders_of_warps_and_ctas(over):
+    """Runs that end `over` entries behind the 128th, 256th, ... entry of the sorted order, and what is left of them."""
+    gen = torch.Generator(device="cuda").manual_seed(over)
+    for lead in (0, 1, 120, 127):
+        counts = [lead, 128 - lead + over, 3, 1, 250, 128 + over, 1, 1, 1, 700, 16, 16]
+        tok = torch.repeat_interleave(torch.arange(len(counts)) * 2, torch.tensor(counts))
+        tok = torch.cat([tok, torch.full((1100,), -1)])[torch.randperm(len(tok) + 1100, generator=torch.Generator().manual_seed(lead))]
+        for width in (264, 7):
+            grad = torch.randn(len(tok), width, generator=gen, device="cuda").half()
+            check(torch.randn(30, width, generator=gen, device="cuda"), tok.cuda(), grad, 0.7)
+
+
 def test_strides_and_shapes():
     gen = torch.Generator(device="cuda").manual_seed(4)
     for width, pad in ((64, 64), (64, 8), (64, 3), (5, 1)):
