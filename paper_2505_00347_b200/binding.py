@@ -7,6 +7,7 @@ there, loading raises: there is no other implementation to fall back to.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import math
 from pathlib import Path
 
@@ -189,6 +190,10 @@ def _stream() -> int:
     if hasattr(torch._C, "_cuda_getDevice"):
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     return handle
+
+
+def _current_device() -> int:
+    return torch._C._cuda_getDevice() if _raw_stream is not None else torch.cuda.current_device()
 
 
 RAW = {"codes_m": 0, "codes_v": 1, "scale_m": 2, "scale_v": 3, "alpha": 4}
@@ -445,8 +450,11 @@ class GradSet:
         _check(lib().solo_grads_create(arr, len(grads), C.byref(self.handle)), "solo_grads_create")
         n = C.c_size_t()
         _check(lib().solo_grads_workspace(self.handle, C.byref(n)), "solo_grads_workspace")
-        self.workspace_floats = -(-n.value // 16) * 4
         self.desc = GradList(self.handle.value, self.ptrs.data_ptr(), _GRAD_DTYPE[dtype])
+        self._ref = C.byref(self.desc)
+        # floats of a call's buffer: workspace, norm, and with every tensor's norm those
+        ws = -(-n.value // 16) * 4
+        self._norm_at, self._lengths = 4 * ws, ([ws, 1], [ws, 1, len(grads)])
 
     def __del__(self):
         try:
@@ -458,7 +466,12 @@ class GradSet:
     def _buffer(self, per_tensor: bool) -> torch.Tensor:
         """A call's workspace, with room for its results after it: from torch's allocator, so that calls on other streams
         and captured graphs have their own."""
-        return torch.empty(self.workspace_floats + 1 + (len(self.sizes) if per_tensor else 0), dtype=torch.float32, device=self.device)
+        return torch.empty(self._norm_at // 4 + (1 + len(self.sizes) if per_tensor else 1), dtype=torch.float32, device=self.device)
+
+    def _results(self, buf: torch.Tensor, per_tensor: bool):
+        if per_tensor:
+            return buf.split(self._lengths[1])[1:]
+        return buf[self._norm_at // 4:]
 
 
 def _norm_type(p) -> int:
@@ -467,26 +480,16 @@ def _norm_type(p) -> int:
     return _NORM_TYPE[p]
 
 
-def _norm_results(ws: torch.Tensor, gs: GradSet, per_tensor: bool):
-    total = ws[gs.workspace_floats:gs.workspace_floats + 1]
-    return (total, ws[gs.workspace_floats + 1:]) if per_tensor else total
-
-
-def _norm_pointers(ws: torch.Tensor, gs: GradSet, per_tensor: bool) -> tuple:
-    base = ws.data_ptr()
-    norm = base + 4 * gs.workspace_floats
-    return norm, norm + 4 if per_tensor else None, base
-
-
 def solo_grad_norm(gs: GradSet, norm_type=2, scale: float = 1.0, per_tensor: bool = False):
     """|scale| times the norm (1, 2 or infinity) of the whole list, as a float32 CUDA tensor of one element; with
     `per_tensor` also one of every tensor's norm.  On the current stream, without waiting, as all of these calls."""
-    ws = gs._buffer(per_tensor)
-    norm, tensors, base = _norm_pointers(ws, gs, per_tensor)
-    rc = (_lib or lib()).solo_grad_norm(C.byref(gs.desc), _norm_type(norm_type), scale, norm, tensors, base, _stream())
+    buf = gs._buffer(per_tensor)
+    base = buf.data_ptr()
+    norm = base + gs._norm_at
+    rc = (_lib or lib()).solo_grad_norm(gs._ref, _norm_type(norm_type), scale, norm, norm + 4 if per_tensor else None, base, _stream())
     if rc:
         _check(rc, "solo_grad_norm")
-    return _norm_results(ws, gs, per_tensor)
+    return gs._results(buf, per_tensor)
 
 
 def solo_grad_clip(src: GradSet, norms, max_norm: float, dst: GradSet = None, norm_type=2, scale: float = 1.0) -> None:
@@ -499,7 +502,7 @@ def solo_grad_clip(src: GradSet, norms, max_norm: float, dst: GradSet = None, no
         n = norms.numel()
         if n == 0:
             raise ValueError("norms has no element")
-    rc = (_lib or lib()).solo_grad_clip(C.byref(src.desc), C.byref((dst or src).desc), norms.data_ptr() if n else None, n,
+    rc = (_lib or lib()).solo_grad_clip(src._ref, (dst or src)._ref, norms.data_ptr() if n else None, n,
                                         _norm_type(norm_type), max_norm if n else 0.0, scale, _stream())
     if rc:
         _check(rc, "solo_grad_clip")
@@ -508,13 +511,14 @@ def solo_grad_clip(src: GradSet, norms, max_norm: float, dst: GradSet = None, no
 def solo_grad_clip_norm(src: GradSet, max_norm: float, dst: GradSet = None, norm_type=2, scale: float = 1.0,
                         per_tensor: bool = False):
     """solo_grad_norm, and solo_grad_clip by its result, in one call; returns what solo_grad_norm does."""
-    ws = src._buffer(per_tensor)
-    norm, tensors, base = _norm_pointers(ws, src, per_tensor)
-    rc = (_lib or lib()).solo_grad_clip_norm(C.byref(src.desc), C.byref((dst or src).desc), _norm_type(norm_type), max_norm,
-                                             scale, norm, tensors, base, _stream())
+    buf = src._buffer(per_tensor)
+    base = buf.data_ptr()
+    norm = base + src._norm_at
+    rc = (_lib or lib()).solo_grad_clip_norm(src._ref, (dst or src)._ref, _norm_type(norm_type), max_norm, scale, norm,
+                                             norm + 4 if per_tensor else None, base, _stream())
     if rc:
         _check(rc, "solo_grad_clip_norm")
-    return _norm_results(ws, src, per_tensor)
+    return src._results(buf, per_tensor)
 
 
 def solo_grad_accumulate(acc: GradSet, grads: GradSet, scale: float = 1.0, first: bool = False, norm_type=None,
@@ -522,34 +526,44 @@ def solo_grad_accumulate(acc: GradSet, grads: GradSet, scale: float = 1.0, first
     """acc (fp32) += scale * grads, or = scale * grads with `first`; with a `norm_type` returns the norm of the new acc
     as solo_grad_norm does, from the same pass."""
     if norm_type is None:
-        rc = (_lib or lib()).solo_grad_accumulate(C.byref(acc.desc), C.byref(grads.desc), scale, 1 if first else 0, -1, None, None,
-                                                  None, _stream())
+        rc = (_lib or lib()).solo_grad_accumulate(acc._ref, grads._ref, scale, 1 if first else 0, -1, None, None, None, _stream())
         if rc:
             _check(rc, "solo_grad_accumulate")
         return None
-    ws = acc._buffer(per_tensor)
-    norm, tensors, base = _norm_pointers(ws, acc, per_tensor)
-    rc = (_lib or lib()).solo_grad_accumulate(C.byref(acc.desc), C.byref(grads.desc), scale, 1 if first else 0,
-                                              _norm_type(norm_type), norm, tensors, base, _stream())
+    buf = acc._buffer(per_tensor)
+    base = buf.data_ptr()
+    norm = base + acc._norm_at
+    rc = (_lib or lib()).solo_grad_accumulate(acc._ref, grads._ref, scale, 1 if first else 0, _norm_type(norm_type), norm,
+                                              norm + 4 if per_tensor else None, base, _stream())
     if rc:
         _check(rc, "solo_grad_accumulate")
-    return _norm_results(ws, acc, per_tensor)
+    return acc._results(buf, per_tensor)
+
 
 _TOKEN_BYTES = {torch.int32: 4, torch.int64: 8}
+
+
+@functools.lru_cache(maxsize=1024)
+def _rows_workspace(num_tokens: int, width: int) -> int:
+    size = C.c_size_t()
+    _check(lib().solo_grad_rows_workspace(num_tokens, width, C.byref(size)), "solo_grad_rows_workspace")
+    return size.value
 
 
 def solo_grad_accumulate_rows(acc: torch.Tensor, tokens: torch.Tensor, grad: torch.Tensor, scale: float = 1.0) -> None:
     """acc[tokens[i], :] += scale * grad[i, :], the gradient of an embedding.  acc: fp32 [rows, width], contiguous; tokens:
     int32 or int64 of any shape, contiguous; grad: fp32, bf16 or fp16 of that shape and a last dimension of width, contiguous
     or, with one dimension of tokens, with rows any distance apart.  Tokens outside the table contribute nothing."""
-    if acc.dim() != 2 or acc.dtype != torch.float32 or not acc.is_contiguous() or not acc.is_cuda:
+    if acc.dim() != 2 or acc.dtype != torch.float32 or not acc.is_cuda or not acc.is_contiguous():
         raise ValueError("acc must be a contiguous float32 CUDA matrix")
     num_rows, width = acc.shape
-    if tokens.dtype not in _TOKEN_BYTES or not tokens.is_contiguous() or tokens.device != acc.device:
+    dev = acc.get_device()
+    if tokens.dtype not in _TOKEN_BYTES or not tokens.is_cuda or tokens.get_device() != dev or not tokens.is_contiguous():
         raise ValueError("tokens must be contiguous int32 or int64 on the accumulator's device")
-    if grad.dtype not in _GRAD_DTYPE or grad.device != acc.device or grad.shape != (*tokens.shape, width):
+    if grad.dtype not in _GRAD_DTYPE or not grad.is_cuda or grad.get_device() != dev or grad.shape != (*tokens.shape, width):
         raise ValueError("grad must be fp32, bf16 or fp16 of the tokens' shape and the accumulator's width, on its device")
-    if acc.device.index != torch.cuda.current_device():
+    stream = _stream()
+    if dev != _current_device():
         raise ValueError("tensors must be on the current device")
     n = tokens.numel()
     if grad.is_contiguous():
@@ -560,13 +574,11 @@ def solo_grad_accumulate_rows(acc: torch.Tensor, tokens: torch.Tensor, grad: tor
         raise ValueError("grad must be contiguous, or a matrix with contiguous rows")
     if n == 0 or num_rows == 0 or width == 0:
         return
-    L = _lib or lib()
-    size = C.c_size_t()
-    _check(L.solo_grad_rows_workspace(n, width, C.byref(size)), "solo_grad_rows_workspace")
-    ws = torch.empty(size.value, dtype=torch.uint8, device=acc.device) if size.value else None
+    size = _rows_workspace(n, width)
+    ws = torch.empty(size, dtype=torch.uint8, device=acc.device) if size else None
     desc = GradRows(acc.data_ptr(), num_rows, width, tokens.data_ptr(), _TOKEN_BYTES[tokens.dtype], _GRAD_DTYPE[grad.dtype],
                     grad.data_ptr(), stride, n)
-    rc = L.solo_grad_accumulate_rows(C.byref(desc), scale, ws.data_ptr() if size.value else None, _stream())
+    rc = (_lib or lib()).solo_grad_accumulate_rows(C.byref(desc), scale, ws.data_ptr() if size else None, stream)
     if rc:
         _check(rc, "solo_grad_accumulate_rows")
 

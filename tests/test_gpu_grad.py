@@ -26,6 +26,9 @@ NORM_TOL = {1: 18 * U, 2: 10 * U, math.inf: U}
 TILE = 8192
 RAGGED = (0, 1, 7, 8, 9, 255, 1000, TILE - 1, TILE, TILE + 1, 0, 0, 3 * TILE + 77, 300, 20 * TILE, 0)
 
+LONG = RAGGED + (1500 * TILE + 5, 0, 17)        # more tiles than CTAs
+LISTS = {"short": RAGGED, "long": LONG}
+
 
 def lib():
     from paper_2505_00347_b200 import binding
@@ -86,7 +89,7 @@ def near_number(got, want, rel):
 @pytest.mark.parametrize("shift", [0, 1, 4])
 def test_norm(p, dtype, shift):
     B = lib()
-    for sizes in (RAGGED, (5,), (0,), (0, 0, 3), (TILE,), (2 * TILE + 3,) * 40):
+    for sizes in (RAGGED, LONG, (5,), (0,), (0, 0, 3), (TILE,), (2 * TILE + 3,) * 40, (2 * TILE + 3,) * 400, (700,) * 3000):
         s = Slab(sizes, DT[dtype], shift).random(3)
         total, per = B.solo_grad_norm(B.GradSet(s.views), norm_type=p, scale=-0.75, per_tensor=True)
         again = B.solo_grad_norm(B.GradSet(s.views), norm_type=p, scale=-0.75)
@@ -160,11 +163,12 @@ def test_clip(src, dst, shifts):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("shift", [0, 1])
-def test_clip_norm_in_place(dtype, shift):
+@pytest.mark.parametrize("sizes", LISTS)
+def test_clip_norm_in_place(dtype, shift, sizes):
     B = lib()
     h = 0.0 if dtype == "f32" else torch.finfo(DT[dtype]).eps / 2
     for p in (1, 2, math.inf):
-        s = Slab(RAGGED, DT[dtype], shift).random(9)
+        s = Slab(LISTS[sizes], DT[dtype], shift).random(9)
         before, N = s.flat(), norm64(s.flat(), p)
         total = B.solo_grad_clip_norm(B.GradSet(s.views), 2.0 * N, norm_type=p)           # below the limit: as it was
         assert torch.equal(s.flat(), before)
@@ -175,12 +179,30 @@ def test_clip_norm_in_place(dtype, shift):
         assert s.untouched()
 
 
+@pytest.mark.parametrize("src,dst", CLIP_PAIRS)
+@pytest.mark.parametrize("sizes", LISTS)
+def test_clip_norm_into_another_list(src, dst, sizes):
+    B = lib()
+    h = 0.0 if dst == "f32" else torch.finfo(DT[dst]).eps / 2
+    for p in (1, 2, math.inf):
+        for shifts in ((0, 0), (0, 4), (3, 3)):
+            s, d = Slab(LISTS[sizes], DT[src], shifts[0]).random(10), Slab(LISTS[sizes], DT[dst], shifts[1])
+            N = 0.125 * norm64(s.flat(), p)
+            limit = float(torch.tensor(0.7 * N))
+            total, per = B.solo_grad_clip_norm(B.GradSet(s.views), limit, dst=B.GradSet(d.views), norm_type=p, scale=0.125, per_tensor=True)
+            near_number(total, N, NORM_TOL[p])
+            near(per, torch.tensor([0.125 * norm64(v, p) for v in s.views], device="cuda", dtype=torch.float64), NORM_TOL[p])
+            near(d.flat(), s.flat() * (0.125 * limit / (N + 1e-6)), h + 3 * U + NORM_TOL[p], HALF_SUBNORMAL[DT[dst]])
+            assert s.untouched() and d.untouched()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("shifts", [(0, 0), (1, 1), (0, 3), (4, 0)])
-def test_accumulate(dtype, shifts):
+@pytest.mark.parametrize("sizes", LISTS)
+def test_accumulate(dtype, shifts, sizes):
     B = lib()
-    acc = Slab(RAGGED, torch.float32, shifts[0]).random(11)
-    g = Slab(RAGGED, DT[dtype], shifts[1]).random(12)
+    acc = Slab(LISTS[sizes], torch.float32, shifts[0]).random(11)
+    g = Slab(LISTS[sizes], DT[dtype], shifts[1]).random(12)
     al, gl = B.GradSet(acc.views), B.GradSet(g.views)
     for p in (None, 1, 2, math.inf):
         for first in (False, True):
@@ -332,7 +354,7 @@ def test_refusals():
         B.GradSet([torch.ones(4, 4, device="cuda")[:, 0]])
     with pytest.raises(ValueError):
         B.GradSet([torch.ones(4, device="cuda", dtype=torch.int32)])
-    ws = torch.empty(a.workspace_floats + 8, device="cuda")
+    ws = torch.empty(a._norm_at // 4 + 8, device="cuda")
     out = torch.zeros(1, device="cuda")
     L, p = B.lib(), B.C.byref(a.desc)
     assert L.solo_grad_norm(p, 2, 1.0, out.data_ptr(), None, ws.data_ptr() + 4, None) == B.SOLO_EALIGN
