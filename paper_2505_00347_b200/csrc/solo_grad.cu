@@ -298,7 +298,7 @@ template <int DS, int DD, bool WRITES> struct Place {
 // ---- the kernel -----------------------------------------------------------------------------------------------------
 
 // DS: type read (gradients); DD: type written; NT: norm type or -1.
-template <int OP, int DS, int DD, int NT> __global__ __launch_bounds__(GCTA, OP == OP_ACC || DS == SOLO_DT_F32 ? (OP == OP_NORM ? 4 : 2) : OP == OP_NORM ? 5 : 4) void grad_kernel(const __grid_constant__ GradArgs a) {
+template <int OP, int DS, int DD, int NT> __global__ __launch_bounds__(GCTA, OP == OP_ACC || DS == SOLO_DT_F32 ? (OP == OP_NORM ? 4 : 2) : OP == OP_NORM ? 5 : 3) void grad_kernel(const __grid_constant__ GradArgs a) {
     using S = std::integral_constant<int, DS>;
     using D = std::integral_constant<int, DD>;
     constexpr bool WRITES = OP != OP_NORM;

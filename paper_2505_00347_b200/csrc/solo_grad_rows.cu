@@ -207,18 +207,52 @@ struct RowsArgs {
     float scale;
 };
 
-template <int DT> __device__ __forceinline__ float row_elem(const void* g, int64_t i) {
-    if constexpr (DT == SOLO_DT_F32) return ((const float*)g)[i];
-    else if constexpr (DT == SOLO_DT_BF16) return __uint_as_float((uint32_t)((const uint16_t*)g)[i] << 16);
-    else return __half2float(((const __half*)g)[i]);
+// Loads that are issued where they are written, so that those of several rows are under way together: a compiler may move a
+// plain one down to where it is used.  With `on` false nothing is loaded and the result is what it was.
+__device__ __forceinline__ void load16_once(uint4& v, const void* p) {
+    asm volatile("ld.global.cs.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+}
+__device__ __forceinline__ void load8_once(uint2& v, const void* p) {
+    asm volatile("ld.global.cs.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p) : "memory");
+}
+__device__ __forceinline__ void load16_acc(float (&v)[4], const float* p, bool on) {
+    asm volatile("{ .reg .pred q; setp.ne.u32 q, %5, 0; @q ld.global.cg.v4.f32 {%0, %1, %2, %3}, [%4]; }"
+                 : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]) : "l"(p), "r"((uint32_t)on) : "memory");
+}
+__device__ __forceinline__ void load4_acc(float& v, const float* p, bool on) {
+    asm volatile("{ .reg .pred q; setp.ne.u32 q, %2, 0; @q ld.global.cg.f32 %0, [%1]; }" : "+f"(v) : "l"(p), "r"((uint32_t)on) : "memory");
+}
+template <int DT> __device__ __forceinline__ float row_elem(const char* g, int64_t i, bool on) {
+    if constexpr (DT == SOLO_DT_F32) {
+        float v = 0.0f;
+        load4_acc(v, (const float*)g + i, on);
+        return v;
+    } else {
+        uint16_t h = 0;
+        asm volatile("{ .reg .pred q; setp.ne.u32 q, %2, 0; @q ld.global.cs.u16 %0, [%1]; }" : "+h"(h) : "l"(g + 2 * i), "r"((uint32_t)on) : "memory");
+        if constexpr (DT == SOLO_DT_BF16) return __uint_as_float((uint32_t)h << 16);
+        else return __half2float(__ushort_as_half(h));
+    }
+}
+// Two sums in one instruction.
+__device__ __forceinline__ void add_pair(float& a, float& b, float x, float y) {
+    asm("{ .reg .b64 s, t; mov.b64 s, {%0, %1}; mov.b64 t, {%2, %3}; add.rn.f32x2 s, s, t; mov.b64 {%0, %1}, s; }" : "+f"(a), "+f"(b) : "f"(x), "f"(y));
 }
 
-// RV columns of a thread: consecutive ones and wide accesses (VEC), or one in every 32.
+// RV columns of a thread: consecutive ones and wide accesses (VEC), or one in every 32.  A thread without columns of its own reads
+// the last ones again and stores nothing.
 template <int DT, bool VEC, int RV> struct Cols {
     static constexpr int WORDS = VEC && DT != SOLO_DT_F32 ? RV / 2 : RV;
     int64_t c0, width;
+    bool some;
+    __device__ __forceinline__ Cols(int64_t slab, int64_t width_) : width(width_) {
+        const int lane = threadIdx.x & 31;
+        c0 = slab * (32 * RV) + (VEC ? lane * RV : lane);
+        some = c0 < width;
+        if (VEC && !some) c0 = width - RV;
+    }
     __device__ __forceinline__ int64_t at(int k) const { return VEC ? c0 + k : c0 + k * 32; }
-    __device__ __forceinline__ bool in(int k) const { return VEC ? c0 < width : at(k) < width; }
+    __device__ __forceinline__ bool in(int k) const { return VEC || at(k) < width; }
     struct Raw { uint32_t w[WORDS]; };
     // of the row that starts at g
     __device__ __forceinline__ Raw load(const char* g) const {
@@ -228,51 +262,48 @@ template <int DT, bool VEC, int RV> struct Cols {
             if constexpr (WORDS % 4 == 0) {
 #pragma unroll
                 for (int q = 0; q < WORDS / 4; ++q) {
-                    const uint4 v = c0 < width ? __ldcs(reinterpret_cast<const uint4*>(p) + q) : make_uint4(0, 0, 0, 0);    // read once
+                    uint4 v;
+                    load16_once(v, p + 16 * q);
                     r.w[4 * q] = v.x; r.w[4 * q + 1] = v.y; r.w[4 * q + 2] = v.z; r.w[4 * q + 3] = v.w;
                 }
             } else {
-                const uint2 v = c0 < width ? __ldcs(reinterpret_cast<const uint2*>(p)) : make_uint2(0, 0);
+                uint2 v;
+                load8_once(v, p);
                 r.w[0] = v.x; r.w[1] = v.y;
             }
         } else {
 #pragma unroll
-            for (int k = 0; k < RV; ++k) r.w[k] = in(k) ? __float_as_uint(row_elem<DT>(g, at(k))) : 0u;
+            for (int k = 0; k < RV; ++k) r.w[k] = __float_as_uint(row_elem<DT>(g, at(k), in(k)));
         }
         return r;
     }
     __device__ __forceinline__ static void add(const Raw& r, float (&s)[RV]) {
-        if constexpr (!VEC || DT == SOLO_DT_F32) {
 #pragma unroll
-            for (int k = 0; k < RV; ++k) s[k] += __uint_as_float(r.w[k]);
-        } else {
-#pragma unroll
-            for (int k = 0; k < RV / 2; ++k) {
-                float2 f;
-                if constexpr (DT == SOLO_DT_BF16) f = make_float2(__uint_as_float(r.w[k] << 16), __uint_as_float(r.w[k] & 0xFFFF0000u));
-                else f = __half22float2(*reinterpret_cast<const __half2*>(&r.w[k]));
-                s[2 * k] += f.x;
-                s[2 * k + 1] += f.y;
-            }
+        for (int k = 0; k < RV / 2; ++k) {
+            float2 f;
+            if constexpr (!VEC || DT == SOLO_DT_F32) f = make_float2(__uint_as_float(r.w[2 * k]), __uint_as_float(r.w[2 * k + 1]));
+            else if constexpr (DT == SOLO_DT_BF16) f = make_float2(__uint_as_float(r.w[k] << 16), __uint_as_float(r.w[k] & 0xFFFF0000u));
+            else f = __half22float2(*reinterpret_cast<const __half2*>(&r.w[k]));
+            add_pair(s[2 * k], s[2 * k + 1], f.x, f.y);
         }
     }
-    __device__ __forceinline__ void load_f32(const float* p, float (&v)[RV]) const {
+    // v is left as it is unless `on`
+    __device__ __forceinline__ void load_f32(const float* p, float (&v)[RV], bool on = true) const {
         if constexpr (VEC) {
-            if (c0 < width) {
 #pragma unroll
-                for (int q = 0; q < RV / 4; ++q) {
-                    const float4 f = __ldcg(reinterpret_cast<const float4*>(p + c0) + q);
-                    v[4 * q] = f.x; v[4 * q + 1] = f.y; v[4 * q + 2] = f.z; v[4 * q + 3] = f.w;
-                }
+            for (int q = 0; q < RV / 4; ++q) {
+                float f[4] = {v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+                load16_acc(f, p + c0 + 4 * q, on);
+                v[4 * q] = f[0]; v[4 * q + 1] = f[1]; v[4 * q + 2] = f[2]; v[4 * q + 3] = f[3];
             }
         } else {
 #pragma unroll
-            for (int k = 0; k < RV; ++k) if (in(k)) v[k] = __ldcg(p + at(k));
+            for (int k = 0; k < RV; ++k) load4_acc(v[k], p + at(k), on && in(k));
         }
     }
     __device__ __forceinline__ void store_f32(float* p, const float (&v)[RV]) const {
         if constexpr (VEC) {
-            if (c0 < width) {
+            if (some) {
 #pragma unroll
                 for (int q = 0; q < RV / 4; ++q)
                     reinterpret_cast<float4*>(p + c0)[q] = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
@@ -348,9 +379,7 @@ template <int DT, bool VEC, int RV> __global__ __launch_bounds__(ROWS_CTA, 4) vo
     const bool continues = some && !(begins >> skip & 1u);              // the first run began before this warp
     const bool goes_on = some && !(ends >> (count - 1) & 1u);           // the last run ends after it
     const bool through = continues && goes_on && ends == 0;             // and these are one
-    Cols<DT, VEC, RV> cols;
-    cols.width = a.width;
-    cols.c0 = (int64_t)slab * SLAB + (VEC ? lane * RV : lane);
+    const Cols<DT, VEC, RV> cols(slab, a.width);
     const uint32_t borders_before = warp == 0 && continues ? border_before(a.tok, c, 0) : NONE;
     const uint32_t borders_after = goes_on ? border_after(a.tok, n, c, 0) : NONE;
     if (threadIdx.x < 2) s.job[threadIdx.x][0] = -1;
@@ -365,39 +394,41 @@ template <int DT, bool VEC, int RV> __global__ __launch_bounds__(ROWS_CTA, 4) vo
     const uint32_t shared_head = continues ? ends & -ends : 0;          // end of a run that began before, if it is here
     const uint32_t whole = ends & ~shared_head;                         // ends of this warp's own runs
     const uint32_t stops = ends | (goes_on ? 1u << (count - 1) : 0u);
-    for (int k = skip; k < count; k += BATCH) {
+    const auto batch = [&](int k, auto full) {
+        constexpr bool FULL = decltype(full)::value;
         typename Cols<DT, VEC, RV>::Raw r[BATCH];
         float v[BATCH][RV];
 #pragma unroll
         for (int b = 0; b < BATCH; ++b) {
-            if (k + b < count) {
-                const typename SumShared<RV>::Entry at = s.entry[warp][k + b];
-                r[b] = cols.load(at.grad);
-                if (whole >> (k + b) & 1u) cols.load_f32(at.row, v[b]);
-            }
+            const int x = FULL ? k + b : min(k + b, count - 1);
+            const typename SumShared<RV>::Entry at = s.entry[warp][x];
+            r[b] = cols.load(at.grad);
+            cols.load_f32(at.row, v[b], whole >> x & 1u);
         }
 #pragma unroll
         for (int b = 0; b < BATCH; ++b) {
             const int x = k + b;
-            if (x < count) {
-                cols.add(r[b], sum);
-                if (stops >> x & 1u) {
-                    if (whole >> x & 1u) {
+            if (!FULL && x >= count) break;
+            cols.add(r[b], sum);
+            if (stops >> x & 1u) {
+                if (whole >> x & 1u) {
 #pragma unroll
-                        for (int q = 0; q < RV; ++q) v[b][q] = __fmaf_rn(a.scale, sum[q], v[b][q]);
-                        cols.store_f32(s.entry[warp][x].row, v[b]);
-                    } else {
-                        // what continues a run: its end, or all of the entries
-                        const int which = shared_head >> x & 1u || through ? 0 : 1;
+                    for (int q = 0; q < RV; ++q) v[b][q] = __fmaf_rn(a.scale, sum[q], v[b][q]);
+                    cols.store_f32(s.entry[warp][x].row, v[b]);
+                } else {
+                    // what continues a run: its end, or all of the entries
+                    const int which = shared_head >> x & 1u || through ? 0 : 1;
 #pragma unroll
-                        for (int q = 0; q < RV; ++q) s.open[which][warp][q][lane] = sum[q];
-                    }
-#pragma unroll
-                    for (int q = 0; q < RV; ++q) sum[q] = 0.0f;
+                    for (int q = 0; q < RV; ++q) s.open[which][warp][q][lane] = sum[q];
                 }
+#pragma unroll
+                for (int q = 0; q < RV; ++q) sum[q] = 0.0f;
             }
         }
-    }
+    };
+    int k = skip;
+    for (; k + BATCH <= count; k += BATCH) batch(k, std::true_type{});
+    if (k < count) batch(k, std::false_type{});
     __syncthreads();
     // Runs of several warps, by the warp that holds the first piece: in this CTA, or (warp 0) of a run from a CTA before.
     for (int side = 0; side < 2; ++side) {
@@ -449,13 +480,15 @@ template <int DT, bool VEC, int RV> __global__ __launch_bounds__(ROWS_CTA, 4) vo
 #pragma unroll
         for (int q = 0; q < RV; ++q) s.join[warp][q][lane] = d[q];
         __syncthreads();
-        double all = 0.0;
+        for (int q = warp; q < RV; q += ROWS_WARPS) {
+            double all = 0.0;
 #pragma unroll
-        for (int u = 0; u < ROWS_WARPS; ++u) all += s.join[u][warp % RV][lane];
-        const int64_t col = (int64_t)slab * SLAB + (VEC ? lane * RV + warp : warp * 32 + lane);
-        if (warp < RV && col < a.width) {
-            float* const at = a.acc + (int64_t)s.job_tok[side] * a.width + col;
-            *at = __fmaf_rn(a.scale, (float)all, *at);
+            for (int u = 0; u < ROWS_WARPS; ++u) all += s.join[u][q][lane];
+            const int64_t col = (int64_t)slab * SLAB + (VEC ? lane * RV + q : q * 32 + lane);
+            if (col < a.width) {
+                float* const at = a.acc + (int64_t)s.job_tok[side] * a.width + col;
+                *at = __fmaf_rn(a.scale, (float)all, *at);
+            }
         }
     }
 }
@@ -502,9 +535,7 @@ template <int DT, bool VEC> __global__ __launch_bounds__(ROWS_CTA) void rows_dir
     if (__any_sync(ALL, found[lane & (ROWS_WARPS - 1)] & 2u)) return;
     const bool alone = (all & (all - 1)) == 0;         // one warp has all the rows
     if (alone && !have) return;
-    Cols<DT, VEC, RV> cols;
-    cols.width = a.width;
-    cols.c0 = (int64_t)slab * SLAB + (VEC ? lane * RV : lane);
+    const Cols<DT, VEC, RV> cols(slab, a.width);
     float* const row = a.acc + t * a.width;
     float old[RV] = {};
     if (alone) cols.load_f32(row, old);
