@@ -222,6 +222,11 @@ __device__ __forceinline__ void load16_acc(float (&v)[4], const float* p, bool o
 __device__ __forceinline__ void load4_acc(float& v, const float* p, bool on) {
     asm volatile("{ .reg .pred q; setp.ne.u32 q, %2, 0; @q ld.global.cg.f32 %0, [%1]; }" : "+f"(v) : "l"(p), "r"((uint32_t)on) : "memory");
 }
+// (what is not loaded here is of no use)
+__device__ __forceinline__ void load16_once(uint4& v, const void* p, bool on) {
+    asm volatile("{ .reg .pred q; setp.ne.u32 q, %5, 0; @q ld.global.cs.v4.u32 {%0, %1, %2, %3}, [%4]; }"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p), "r"((uint32_t)on) : "memory");
+}
 template <int DT> __device__ __forceinline__ float row_elem(const char* g, int64_t i, bool on) {
     if constexpr (DT == SOLO_DT_F32) {
         float v = 0.0f;
@@ -255,7 +260,7 @@ template <int DT, bool VEC, int RV> struct Cols {
     __device__ __forceinline__ bool in(int k) const { return VEC || at(k) < width; }
     struct Raw { uint32_t w[WORDS]; };
     // of the row that starts at g
-    __device__ __forceinline__ Raw load(const char* g) const {
+    template <class... On> __device__ __forceinline__ Raw load(const char* g, On... on) const {
         Raw r;
         if constexpr (VEC) {
             const char* const p = g + c0 * (DT == SOLO_DT_F32 ? 4 : 2);
@@ -263,7 +268,7 @@ template <int DT, bool VEC, int RV> struct Cols {
 #pragma unroll
                 for (int q = 0; q < WORDS / 4; ++q) {
                     uint4 v;
-                    load16_once(v, p + 16 * q);
+                    load16_once(v, p + 16 * q, on...);
                     r.w[4 * q] = v.x; r.w[4 * q + 1] = v.y; r.w[4 * q + 2] = v.z; r.w[4 * q + 3] = v.w;
                 }
             } else {
@@ -273,7 +278,7 @@ template <int DT, bool VEC, int RV> struct Cols {
             }
         } else {
 #pragma unroll
-            for (int k = 0; k < RV; ++k) r.w[k] = __float_as_uint(row_elem<DT>(g, at(k), in(k)));
+            for (int k = 0; k < RV; ++k) r.w[k] = __float_as_uint(row_elem<DT>(g, at(k), (in(k) && ... && on)));
         }
         return r;
     }
@@ -507,7 +512,7 @@ struct DirectArgs {
 };
 
 template <int DT, bool VEC> __global__ __launch_bounds__(ROWS_CTA) void rows_direct_kernel(const __grid_constant__ DirectArgs a) {
-    constexpr int RV = WIDE, SLAB = 32 * RV;
+    constexpr int RV = WIDE, SLAB = 32 * RV, ES = DT == SOLO_DT_F32 ? 4 : 2;
     constexpr uint32_t ALL = 0xFFFFFFFFu;
     __shared__ float part[ROWS_WARPS][RV][32];
     __shared__ uint32_t found[ROWS_WARPS];             // 1: the token is among the warp's, 2: before this CTA's
@@ -545,18 +550,21 @@ template <int DT, bool VEC> __global__ __launch_bounds__(ROWS_CTA) void rows_dir
     for (int k = 0; k < DIRECT_WORDS; ++k) {
         float sum[RV] = {};
         uint32_t left = m[k];
+        const char* const rows = (const char*)a.grad + (warp * words + k) * 32 * a.grad_stride * ES;
         while (left) {
             typename Cols<DT, VEC, RV>::Raw r[BATCH];
-            bool on[BATCH];
+            uint32_t after = left;
 #pragma unroll
             for (int b = 0; b < BATCH; ++b) {
-                on[b] = left != 0;
-                if (on[b]) r[b] = cols.load((const char*)a.grad + ((warp * words + k) * 32 + __ffs(left) - 1) * a.grad_stride * (DT == SOLO_DT_F32 ? 4 : 2));
-                left &= left - 1;
+                r[b] = cols.load(rows + max(__ffs(after) - 1, 0) * a.grad_stride * ES, after != 0);
+                after &= after - 1;
             }
 #pragma unroll
-            for (int b = 0; b < BATCH; ++b)
-                if (on[b]) cols.add(r[b], sum);
+            for (int b = 0; b < BATCH; ++b) {
+                if (left == 0) break;
+                cols.add(r[b], sum);
+                left &= left - 1;
+            }
         }
 #pragma unroll
         for (int q = 0; q < RV; ++q) total[q] += sum[q];
