@@ -410,10 +410,14 @@ enum { SOLO_NORM_MAX = 0, SOLO_NORM_1 = 1, SOLO_NORM_2 = 2 };      /* max |g|, s
  * any number of calls, streams and captured graphs may use it at once; it has to outlive them. */
 typedef struct solo_grads solo_grads_t;
 
-/* `numel_host` is a HOST array; 0 is allowed (an empty tensor), and so are lists with no element at all.  Synchronous
- * (cudaMalloc, cudaMemcpy). */
-int solo_grads_create(const int64_t* numel_host, int num_tensors, solo_grads_t** out);
-/* Synchronizes the device and frees the sizes.  NULL is accepted. */
+/*
+ * `numel_host` is a HOST array; 0 is allowed (an empty tensor), and so are lists with no element at all.
+ * `geom_dev` is device memory of 2 * num_tensors + 1 int64 that the caller keeps as long as the handle: the call fills it
+ * on `stream` (the values are staged before it returns), and work on other streams has to be ordered after that.  Not while
+ * `stream` is capturing (SOLO_EINVAL).  None of the calls on gradients allocates device memory or waits for the device.
+ */
+int solo_grads_create(const int64_t* numel_host, int num_tensors, int64_t* geom_dev, void* stream, solo_grads_t** out);
+/* Frees the handle's host memory.  NULL is accepted. */
 int solo_grads_destroy(solo_grads_t* grads);
 /* Bytes of the workspace that the calls with a norm need (16-byte aligned device memory).  Its contents
  * do not matter before a call nor last after it; calls that may run at the same time need one each. */
@@ -445,7 +449,7 @@ int solo_grad_norm(const solo_grad_list_t* list, int norm_type, float scale, flo
  * norms of the scaled gradients, as solo_grad_norm gives them.  num_norms = 0: f = scale, a plain
  * scaling or conversion.  `dst` may be `src` (in place; nothing is read or written then if f is 1) or
  * a list of the same sizes and any type.  A norm that is NaN makes everything NaN, an infinite one
- * finite gradients 0; max_norm is finite and not negative.
+ * finite gradients 0; max_norm is finite and not negative.  No tensor of `dst` overlaps another one.
  */
 int solo_grad_clip(const solo_grad_list_t* src, const solo_grad_list_t* dst, const float* norms_dev,
                    int num_norms, int norm_type, float max_norm, float scale, void* stream);
@@ -457,7 +461,7 @@ int solo_grad_clip_norm(const solo_grad_list_t* src, const solo_grad_list_t* dst
 
 /*
  * acc = acc + scale * g, or scale * g with `first` (acc is not read then), one rounding for each
- * element; `acc` is a list of binary32 tensors of the same sizes.  norm_type -1: nothing else
+ * element; `acc` is a list of binary32 tensors of the same sizes, none of which overlaps another one.  norm_type -1: nothing else
  * (norm_dev, tensor_norm_dev and workspace_dev are not used); otherwise also the norm of the new acc, from
  * the same pass.
  */

@@ -146,7 +146,7 @@ def lib() -> C.CDLL:
     L.solo_launch_count.restype = C.c_int64
     L.solo_strerror.argtypes = [i32]
     gl, f32 = C.POINTER(GradList), C.c_float
-    L.solo_grads_create.argtypes = [C.POINTER(C.c_int64), i32, C.POINTER(vp)]
+    L.solo_grads_create.argtypes = [C.POINTER(C.c_int64), i32, vp, vp, C.POINTER(vp)]
     L.solo_grads_destroy.argtypes = [vp]
     L.solo_grads_workspace.argtypes = [vp, C.POINTER(C.c_size_t)]
     L.solo_grad_norm.argtypes = [gl, i32, f32, vp, vp, vp, vp]
@@ -429,7 +429,9 @@ _NORM_TYPE = {math.inf: 0, 1: 1, 2: 2}
 
 
 class GradSet:
-    """Descriptor of a list of gradient tensors of one type: fp32, bf16 or fp16 (built once, reused every step)."""
+    """Descriptor of a list of gradient tensors of one type: fp32, bf16 or fp16 (built once, reused every step).  Made on the
+    current stream; work on other streams is ordered after that by the caller.  It outlives the work and the captured graphs
+    that use it, as the tensors do."""
 
     def __init__(self, grads: list[torch.Tensor]):
         if not grads:
@@ -444,10 +446,15 @@ class GradSet:
             raise ValueError("gradients must be on the current device")
         self.grads, self.dtype, self.device = list(grads), dtype, dev
         self.sizes = [g.numel() for g in grads]
-        self.ptrs = torch.tensor([g.data_ptr() for g in grads], dtype=torch.int64, device=dev)
+        ptrs = [g.data_ptr() for g in grads]
+        self.ptrs = torch.tensor(ptrs, dtype=torch.int64, device=dev)
+        self.geom = torch.empty(2 * len(grads) + 1, dtype=torch.int64, device=dev)
         self.handle = C.c_void_p()
         arr = (C.c_int64 * len(grads))(*self.sizes)
-        _check(lib().solo_grads_create(arr, len(grads), C.byref(self.handle)), "solo_grads_create")
+        _check(lib().solo_grads_create(arr, len(grads), self.geom.data_ptr(), _stream(), C.byref(self.handle)), "solo_grads_create")
+        # a list that is written must not have two tensors over the same memory
+        ends = sorted((p, p + n * grads[0].element_size()) for p, n in zip(ptrs, self.sizes) if n)
+        self._apart = all(a[1] <= b[0] for a, b in zip(ends, ends[1:]))
         n = C.c_size_t()
         _check(lib().solo_grads_workspace(self.handle, C.byref(n)), "solo_grads_workspace")
         self.desc = GradList(self.handle.value, self.ptrs.data_ptr(), _GRAD_DTYPE[dtype])
@@ -474,6 +481,12 @@ class GradSet:
         return buf[self._norm_at // 4:]
 
 
+def _written(gs: GradSet):
+    if not gs._apart:
+        raise ValueError("tensors of a list that is written must not overlap")
+    return gs._ref
+
+
 def _norm_type(p) -> int:
     if p not in _NORM_TYPE:
         raise ValueError("norm_type must be 1, 2 or infinity")
@@ -497,12 +510,12 @@ def solo_grad_clip(src: GradSet, norms, max_norm: float, dst: GradSet = None, no
     `norms` of its parts (a float32 CUDA tensor); norms=None: scaling and conversion alone."""
     n = 0
     if norms is not None:
-        if not norms.is_cuda or norms.dtype != torch.float32 or not norms.is_contiguous() or norms.device != src.device:
+        if not isinstance(norms, torch.Tensor) or not norms.is_cuda or norms.dtype != torch.float32 or not norms.is_contiguous() or norms.device != src.device:
             raise ValueError("norms must be a contiguous float32 tensor on the gradients' device")
         n = norms.numel()
         if n == 0:
             raise ValueError("norms has no element")
-    rc = (_lib or lib()).solo_grad_clip(src._ref, (dst or src)._ref, norms.data_ptr() if n else None, n,
+    rc = (_lib or lib()).solo_grad_clip(src._ref, _written(dst or src), norms.data_ptr() if n else None, n,
                                         _norm_type(norm_type), max_norm if n else 0.0, scale, _stream())
     if rc:
         _check(rc, "solo_grad_clip")
@@ -514,7 +527,7 @@ def solo_grad_clip_norm(src: GradSet, max_norm: float, dst: GradSet = None, norm
     buf = src._buffer(per_tensor)
     base = buf.data_ptr()
     norm = base + src._norm_at
-    rc = (_lib or lib()).solo_grad_clip_norm(src._ref, (dst or src)._ref, _norm_type(norm_type), max_norm, scale, norm,
+    rc = (_lib or lib()).solo_grad_clip_norm(src._ref, _written(dst or src), _norm_type(norm_type), max_norm, scale, norm,
                                              norm + 4 if per_tensor else None, base, _stream())
     if rc:
         _check(rc, "solo_grad_clip_norm")
@@ -526,14 +539,14 @@ def solo_grad_accumulate(acc: GradSet, grads: GradSet, scale: float = 1.0, first
     """acc (fp32) += scale * grads, or = scale * grads with `first`; with a `norm_type` returns the norm of the new acc
     as solo_grad_norm does, from the same pass."""
     if norm_type is None:
-        rc = (_lib or lib()).solo_grad_accumulate(acc._ref, grads._ref, scale, 1 if first else 0, -1, None, None, None, _stream())
+        rc = (_lib or lib()).solo_grad_accumulate(_written(acc), grads._ref, scale, 1 if first else 0, -1, None, None, None, _stream())
         if rc:
             _check(rc, "solo_grad_accumulate")
         return None
     buf = acc._buffer(per_tensor)
     base = buf.data_ptr()
     norm = base + acc._norm_at
-    rc = (_lib or lib()).solo_grad_accumulate(acc._ref, grads._ref, scale, 1 if first else 0, _norm_type(norm_type), norm,
+    rc = (_lib or lib()).solo_grad_accumulate(_written(acc), grads._ref, scale, 1 if first else 0, _norm_type(norm_type), norm,
                                               norm + 4 if per_tensor else None, base, _stream())
     if rc:
         _check(rc, "solo_grad_accumulate")

@@ -3,14 +3,14 @@
 // All of these are streams over ragged lists of tensors, a read of 2 or 4 bytes per element and up to
 // 8 bytes written and read besides, and one or two operations on it: bound by HBM.  One kernel template serves them.  The list
 // is cut into tiles of 8192 elements of one tensor each.  The CTAs, as many as are resident, take the tiles in turn, so that all
-// of them work on one stretch of memory (clip of the 125M-parameter set 89 -> 79 us against a contiguous share each); where every tensor's
+// of them work on one stretch of memory (clip of the 125M-parameter set in place: 79 us, with a contiguous share each 89); where every tensor's
 // norm is wanted a CTA takes a contiguous share instead, so that its sums need one partial for each tensor that it touches.
 // What the next tile is gets looked up while the loads of the present one are under way.
 //
 // Sums.  A thread sums the (at most 32) powers that it takes from a tile in binary32 and adds that to a binary64 sum;
 // threads, CTAs and tensors are summed in binary64 in a fixed order (no atomics), so results do not vary from call to call.
 // A binary32 sum that overflowed, or is so small that squares may have been lost below 2^-149, is taken again in binary64
-// from the values still in registers.  Maxima are maxima of magnitude bit patterns, above all of which NaN lies.
+// from the values in memory.  Maxima are maxima of magnitude bit patterns, above all of which NaN lies.
 #include "solo.h"
 
 #include <cuda_bf16.h>
@@ -548,7 +548,7 @@ struct solo_grads {
     int num_tensors = 0;
     int64_t tiles = 0;
     std::vector<int64_t> numel;
-    int64_t* geom = nullptr;      // device: numel[T] | tile_start[T + 1]
+    const int64_t* geom = nullptr;  // device, the caller's: numel[T] | tile_start[T + 1]
 };
 
 namespace {
@@ -638,44 +638,52 @@ GradArgs norm_args(const solo_grads* g, void* workspace, const float* tensor_nor
 
 extern "C" {
 
-int solo_grads_create(const int64_t* numel_host, int num_tensors, solo_grads_t** out) {
+int solo_grads_create(const int64_t* numel_host, int num_tensors, int64_t* geom_dev, void* stream_, solo_grads_t** out) {
     if (!out) return SOLO_EINVAL;
     *out = nullptr;
-    if (!numel_host || num_tensors < 1) return SOLO_EINVAL;
-    for (int t = 0; t < num_tensors; ++t)
+    if (!numel_host || !geom_dev || num_tensors < 1) return SOLO_EINVAL;
+    if ((uintptr_t)geom_dev & 7u) return SOLO_EALIGN;
+    int64_t tiles = 0;
+    for (int t = 0; t < num_tensors; ++t) {
         if (numel_host[t] < 0 || numel_host[t] > ((int64_t)1 << 48)) return SOLO_EINVAL;
+        tiles += (numel_host[t] + GTILE - 1) / GTILE;
+        if (tiles > ((int64_t)1 << 40)) return SOLO_EINVAL;             // share arithmetic: tiles * CTAs in 64 bits
+    }
+    cudaStream_t stream = (cudaStream_t)stream_;
+    int device = -1;
+    cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;          // the copy below is from this call's memory
+    if (cudaGetDevice(&device) != cudaSuccess || cudaStreamIsCapturing(stream, &cap) != cudaSuccess) { cudaGetLastError(); return SOLO_ECUDA; }
+    if (cap != cudaStreamCaptureStatusNone) return SOLO_EINVAL;
     solo_grads* g = nullptr;
     try {
         g = new solo_grads();
         g->numel.assign(numel_host, numel_host + num_tensors);
         std::vector<int64_t> geom(g->numel);
+        geom.reserve(2 * (size_t)num_tensors + 1);
+        int64_t at = 0;
         for (int t = 0; t < num_tensors; ++t) {
-            geom.push_back(g->tiles);
-            g->tiles += (numel_host[t] + GTILE - 1) / GTILE;
+            geom.push_back(at);
+            at += (numel_host[t] + GTILE - 1) / GTILE;
         }
-        geom.push_back(g->tiles);
-        g->num_tensors = num_tensors;
-        if (g->tiles > ((int64_t)1 << 40)) { delete g; return SOLO_EINVAL; }       // share arithmetic: tiles * CTAs in 64 bits
-        if (cudaGetDevice(&g->device) != cudaSuccess) { cudaGetLastError(); delete g; return SOLO_ECUDA; }
-        if (cudaMalloc((void**)&g->geom, geom.size() * 8) != cudaSuccess) { cudaGetLastError(); delete g; return SOLO_ENOMEM; }
-        if (cudaMemcpy(g->geom, geom.data(), geom.size() * 8, cudaMemcpyHostToDevice) != cudaSuccess) {
+        geom.push_back(at);
+        if (cudaMemcpyAsync(geom_dev, geom.data(), geom.size() * 8, cudaMemcpyHostToDevice, stream) != cudaSuccess) {
             cudaGetLastError();
-            cudaFree(g->geom);
             delete g;
             return SOLO_ECUDA;
         }
     } catch (const std::bad_alloc&) {
-        if (g) delete g;
+        delete g;
         return SOLO_ENOMEM;
     }
+    g->device = device;
+    g->num_tensors = num_tensors;
+    g->tiles = tiles;
+    g->geom = geom_dev;
     *out = g;
     return SOLO_OK;
 }
 
 int solo_grads_destroy(solo_grads_t* g) {
-    if (!g) return SOLO_OK;
-    cudaDeviceSynchronize();
-    cudaFree(g->geom);
     delete g;
     return SOLO_OK;
 }

@@ -307,6 +307,23 @@ def test_on_another_stream_and_in_graphs():
         near(d.flat(), s.flat() * min(1.0, 0.125 * (k + 1) / (N + 1e-6)), 12 * U, 2.0 ** -150)
 
 
+def test_an_accumulator_as_its_own_gradient_and_lists_made_while_capturing():
+    B = lib()
+    x = torch.randn(3 * TILE + 11, device="cuda")
+    gs, before = B.GradSet([x]), x.clone()
+    B.solo_grad_accumulate(gs, gs, scale=0.5)
+    near(x, before.double() * 1.5, U)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        with pytest.raises(B.SoloError) as e:
+            arr, h = (B.C.c_int64 * 1)(4), B.C.c_void_p()
+            B._check(B.lib().solo_grads_create(arr, 1, gs.geom.data_ptr(), B._stream(), B.C.byref(h)), "solo_grads_create")
+        del gs                                                          # nothing of a list's end disturbs a capture
+    assert e.value.status == B.SOLO_EINVAL
+    graph.replay()
+    torch.cuda.synchronize()
+
+
 def test_a_tensor_beyond_32_bit_offsets():
     B = lib()
     n = (1 << 31) + 12345
@@ -345,7 +362,15 @@ def test_refusals():
         refused(B.SOLO_EINVAL, lambda: B.solo_grad_clip(a, one, 1.0, scale=bad))
         refused(B.SOLO_EINVAL, lambda: B.solo_grad_clip_norm(a, 1.0, scale=bad))
         refused(B.SOLO_EINVAL, lambda: B.solo_grad_accumulate(a, a, scale=bad))
-    for norms in (one.cpu(), one.double(), torch.ones(2, 2, device="cuda")[:, 0], one[:0]):
+    for bad in (B.GradSet([x, x]), B.GradSet([x[:50], x[40:]])):               # memory written twice
+        with pytest.raises(ValueError):
+            B.solo_grad_clip(bad, one, 1.0)
+        with pytest.raises(ValueError):
+            B.solo_grad_clip_norm(bad, 1.0)
+        with pytest.raises(ValueError):
+            B.solo_grad_accumulate(bad, bad)
+    assert float(B.solo_grad_norm(B.GradSet([x, x]), norm_type=1)) == 200.0
+    for norms in (2.0, one.cpu(), one.double(), torch.ones(2, 2, device="cuda")[:, 0], one[:0]):
         with pytest.raises(ValueError):
             B.solo_grad_clip(a, norms, 1.0)
     with pytest.raises(ValueError):

@@ -12,18 +12,19 @@ def B():
     return binding
 
 
-def create(B, sizes, n=None):
+def create(B, sizes, n=None, geom=256):
     h = C.c_void_p(1)
     arr = (C.c_int64 * max(1, len(sizes)))(*sizes)
-    return B.lib().solo_grads_create(arr, len(sizes) if n is None else n, C.byref(h)), h
+    return B.lib().solo_grads_create(arr, len(sizes) if n is None else n, geom, None, C.byref(h)), h
 
 
 def test_sizes_are_checked(B):
-    for sizes, n in (([], None), ([1], -1), ([-1], None), ([5, -3], None), ([(1 << 48) + 1], None)):
+    for sizes, n in (([], None), ([1], -1), ([-1], None), ([5, -3], None), ([(1 << 48) + 1], None), ([1 << 48] * 40, None)):
         rc, h = create(B, sizes, n)
         assert rc == B.SOLO_EINVAL and not h.value, (sizes, n)
-    assert B.lib().solo_grads_create(None, 1, C.byref(C.c_void_p())) == B.SOLO_EINVAL
-    assert B.lib().solo_grads_create((C.c_int64 * 1)(4), 1, None) == B.SOLO_EINVAL
+    assert create(B, [4], geom=None)[0] == B.SOLO_EINVAL and create(B, [4], geom=260)[0] == B.SOLO_EALIGN
+    assert B.lib().solo_grads_create(None, 1, 256, None, C.byref(C.c_void_p())) == B.SOLO_EINVAL
+    assert B.lib().solo_grads_create((C.c_int64 * 1)(4), 1, 256, None, None) == B.SOLO_EINVAL
     assert B.lib().solo_grads_destroy(None) == B.SOLO_OK
     assert B.lib().solo_grads_workspace(None, C.byref(C.c_size_t())) == B.SOLO_EINVAL
 
