@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes as C
 import functools
 import math
+import weakref
 from pathlib import Path
 
 import torch
@@ -439,22 +440,25 @@ class GradSet:
         dtype, dev = grads[0].dtype, grads[0].device
         if dtype not in _GRAD_DTYPE:
             raise ValueError("gradients must be fp32, bf16 or fp16")
+        index = dev.index
         for g in grads:
-            if not (g.is_cuda and g.is_contiguous()) or g.dtype != dtype or g.device != dev:
+            if not (g.is_cuda and g.is_contiguous()) or g.dtype != dtype or g.get_device() != index:
                 raise ValueError("gradients must be contiguous CUDA tensors of one type on one device")
-        if dev.index != torch.cuda.current_device():
+        if index != torch.cuda.current_device():
             raise ValueError("gradients must be on the current device")
         self.grads, self.dtype, self.device = list(grads), dtype, dev
         self.sizes = [g.numel() for g in grads]
         ptrs = [g.data_ptr() for g in grads]
-        self.ptrs = torch.tensor(ptrs, dtype=torch.int64, device=dev)
+        self.ptrs = torch.tensor(ptrs, dtype=torch.int64).to(dev, non_blocking=True)      # staged before it returns
         self.geom = torch.empty(2 * len(grads) + 1, dtype=torch.int64, device=dev)
         self.handle = C.c_void_p()
         arr = (C.c_int64 * len(grads))(*self.sizes)
         _check(lib().solo_grads_create(arr, len(grads), self.geom.data_ptr(), _stream(), C.byref(self.handle)), "solo_grads_create")
         # a list that is written must not have two tensors over the same memory
-        ends = sorted((p, p + n * grads[0].element_size()) for p, n in zip(ptrs, self.sizes) if n)
-        self._apart = all(a[1] <= b[0] for a, b in zip(ends, ends[1:]))
+        self._spans = [(p, p + n * grads[0].element_size()) for p, n in zip(ptrs, self.sizes) if n]
+        self._apart = _disjoint(sorted(self._spans))
+        self._low, self._high = min((a for a, _ in self._spans), default=0), max((b for _, b in self._spans), default=0)
+        self._clear_of = {}           # lists that this one was found to lie clear of, by id
         n = C.c_size_t()
         _check(lib().solo_grads_workspace(self.handle, C.byref(n)), "solo_grads_workspace")
         self.desc = GradList(self.handle.value, self.ptrs.data_ptr(), _GRAD_DTYPE[dtype])
@@ -481,9 +485,31 @@ class GradSet:
         return buf[self._norm_at // 4:]
 
 
-def _written(gs: GradSet):
+def _disjoint(spans) -> bool:
+    return all(a[1] <= b[0] for a, b in zip(spans, spans[1:]))
+
+
+def _union(spans) -> list:
+    out = []
+    for a, b in sorted(spans):
+        if out and a <= out[-1][1]:
+            out[-1] = (out[-1][0], max(b, out[-1][1]))
+        else:
+            out.append((a, b))
+    return out
+
+
+def _written(gs: GradSet, read: GradSet):
+    """gs as the list that a call writes while it reads `read`: the same tensors in the same type, or none of their memory."""
     if not gs._apart:
         raise ValueError("tensors of a list that is written must not overlap")
+    if read is not gs and read._low < gs._high and gs._low < read._high:
+        known = gs._clear_of.get(id(read))
+        if known is None or known() is not read:
+            same = read._spans == gs._spans and read.dtype == gs.dtype
+            if not same and not _disjoint(sorted(gs._spans + _union(read._spans))):
+                raise ValueError("the lists of a call must not overlap, unless they are the same")
+            gs._clear_of[id(read)] = weakref.ref(read)
     return gs._ref
 
 
@@ -515,7 +541,7 @@ def solo_grad_clip(src: GradSet, norms, max_norm: float, dst: GradSet = None, no
         n = norms.numel()
         if n == 0:
             raise ValueError("norms has no element")
-    rc = (_lib or lib()).solo_grad_clip(src._ref, _written(dst or src), norms.data_ptr() if n else None, n,
+    rc = (_lib or lib()).solo_grad_clip(src._ref, _written(dst or src, src), norms.data_ptr() if n else None, n,
                                         _norm_type(norm_type), max_norm if n else 0.0, scale, _stream())
     if rc:
         _check(rc, "solo_grad_clip")
@@ -527,7 +553,7 @@ def solo_grad_clip_norm(src: GradSet, max_norm: float, dst: GradSet = None, norm
     buf = src._buffer(per_tensor)
     base = buf.data_ptr()
     norm = base + src._norm_at
-    rc = (_lib or lib()).solo_grad_clip_norm(src._ref, _written(dst or src), _norm_type(norm_type), max_norm, scale, norm,
+    rc = (_lib or lib()).solo_grad_clip_norm(src._ref, _written(dst or src, src), _norm_type(norm_type), max_norm, scale, norm,
                                              norm + 4 if per_tensor else None, base, _stream())
     if rc:
         _check(rc, "solo_grad_clip_norm")
@@ -539,14 +565,14 @@ def solo_grad_accumulate(acc: GradSet, grads: GradSet, scale: float = 1.0, first
     """acc (fp32) += scale * grads, or = scale * grads with `first`; with a `norm_type` returns the norm of the new acc
     as solo_grad_norm does, from the same pass."""
     if norm_type is None:
-        rc = (_lib or lib()).solo_grad_accumulate(_written(acc), grads._ref, scale, 1 if first else 0, -1, None, None, None, _stream())
+        rc = (_lib or lib()).solo_grad_accumulate(_written(acc, grads), grads._ref, scale, 1 if first else 0, -1, None, None, None, _stream())
         if rc:
             _check(rc, "solo_grad_accumulate")
         return None
     buf = acc._buffer(per_tensor)
     base = buf.data_ptr()
     norm = base + acc._norm_at
-    rc = (_lib or lib()).solo_grad_accumulate(_written(acc), grads._ref, scale, 1 if first else 0, _norm_type(norm_type), norm,
+    rc = (_lib or lib()).solo_grad_accumulate(_written(acc, grads), grads._ref, scale, 1 if first else 0, _norm_type(norm_type), norm,
                                               norm + 4 if per_tensor else None, base, _stream())
     if rc:
         _check(rc, "solo_grad_accumulate")

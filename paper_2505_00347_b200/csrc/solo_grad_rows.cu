@@ -61,7 +61,7 @@ struct SortShared {
     uint32_t scan[SORT_WARPS];
 };
 
-// The time goes into latencies (16,384 tokens, two passes: 1024 threads in eight CTAs 12.5 us, 256 threads in sixteen @@ us).
+// The time goes into latencies (16,384 tokens, two passes: 1024 threads in eight CTAs 12.5 us, 256 threads in sixteen 9.6 us).
 // ROUNDS: tokens per thread, at most; BITS: of a digit, at most.
 template <int ROUNDS, int BITS> __global__ __launch_bounds__(SORT_CTA) void rows_sort_kernel(const __grid_constant__ SortArgs a) {
     constexpr uint32_t ALL = 0xFFFFFFFFu, NONE = 0xFFFFFFFFu;

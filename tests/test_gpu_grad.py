@@ -370,6 +370,22 @@ def test_refusals():
         with pytest.raises(ValueError):
             B.solo_grad_accumulate(bad, bad)
     assert float(B.solo_grad_norm(B.GradSet([x, x]), norm_type=1)) == 200.0
+    z = torch.ones(300, device="cuda")
+    lists = {k: B.GradSet(v) for k, v in dict(first=[z[:100], z[200:]], swapped=[z[200:], z[:100]],
+                                              late=[z[4:104], z[200:]], between=[z[100:150], z[150:200]]).items()}
+    for other in ("swapped", "late"):                                            # other tensors, some of the same memory
+        for _ in range(2):
+            with pytest.raises(ValueError):
+                B.solo_grad_clip(lists["first"], None, 0.0, dst=lists[other])
+            with pytest.raises(ValueError):
+                B.solo_grad_accumulate(lists[other], lists["first"])
+    again = B.GradSet([z[:100], z[200:]])
+    for _ in range(2):
+        B.solo_grad_clip(lists["first"], None, 0.0, dst=again, scale=2.0)          # the same tensors
+        B.solo_grad_clip(B.GradSet([z[:50], z[200:250]]), None, 0.0, dst=lists["between"], scale=0.5)    # between them
+    assert z[:100].eq(4).all() and z[200:].eq(4).all() and z[100:200].eq(2).all()
+    B.solo_grad_clip(B.GradSet([z[:50], z[:50]]), None, 0.0, dst=lists["between"])  # read twice: no matter
+    assert z[100:200].eq(4).all()
     for norms in (2.0, one.cpu(), one.double(), torch.ones(2, 2, device="cuda")[:, 0], one[:0]):
         with pytest.raises(ValueError):
             B.solo_grad_clip(a, norms, 1.0)
