@@ -419,8 +419,9 @@ typedef struct solo_grads solo_grads_t;
 int solo_grads_create(const int64_t* numel_host, int num_tensors, int64_t* geom_dev, void* stream, solo_grads_t** out);
 /* Frees the handle's host memory.  NULL is accepted. */
 int solo_grads_destroy(solo_grads_t* grads);
-/* Bytes of the workspace that the calls with a norm need (16-byte aligned device memory).  Its contents
- * do not matter before a call nor last after it; calls that may run at the same time need one each. */
+/* Bytes of the workspace that the calls with a norm need (16-byte aligned device memory).  Its first 16 bytes are zero before
+ * its first use, and every call leaves them so; the rest may hold anything, and in a call that is captured all of it.  Calls that may run at the same time need one
+ * each; so do threads that call on one stream without taking turns. */
 int solo_grads_workspace(const solo_grads_t* grads, size_t* bytes);
 
 /*
@@ -487,7 +488,8 @@ typedef struct {
     int64_t grad_stride;         /* >= 0 */
     int64_t num_tokens;          /* 0 .. 2^40 */
 } solo_grad_rows_t;
-/* `workspace_dev`: 16-byte aligned device memory of solo_grad_rows_workspace's size, as for solo_grads_workspace; NULL if that is 0. */
+/* `workspace_dev`: 16-byte aligned device memory of solo_grad_rows_workspace's size, NULL if that is 0.  It may hold anything; calls
+ * that may run at the same time need one each. */
 int solo_grad_rows_workspace(int64_t num_tokens, int64_t width, size_t* bytes);
 int solo_grad_accumulate_rows(const solo_grad_rows_t* rows, float scale, void* workspace_dev, void* stream);
 

@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes as C
 import functools
 import math
+import threading
 import weakref
 from pathlib import Path
 
@@ -463,9 +464,9 @@ class GradSet:
         _check(lib().solo_grads_workspace(self.handle, C.byref(n)), "solo_grads_workspace")
         self.desc = GradList(self.handle.value, self.ptrs.data_ptr(), _GRAD_DTYPE[dtype])
         self._ref = C.byref(self.desc)
-        # floats of a call's buffer: workspace, norm, and with every tensor's norm those
-        ws = -(-n.value // 16) * 4
-        self._norm_at, self._lengths = 4 * ws, ([ws, 1], [ws, 1, len(grads)])
+        self._workspace_bytes = n.value
+        self._workspaces = {}         # by stream: calls on one stream follow one another
+        self._turn = threading.Lock()
 
     def __del__(self):
         try:
@@ -474,15 +475,17 @@ class GradSet:
         except Exception:
             pass
 
-    def _buffer(self, per_tensor: bool) -> torch.Tensor:
-        """A call's workspace, with room for its results after it: from torch's allocator, so that calls on other streams
-        and captured graphs have their own."""
-        return torch.empty(self._norm_at // 4 + (1 + len(self.sizes) if per_tensor else 1), dtype=torch.float32, device=self.device)
+    def _workspace(self, stream: int) -> torch.Tensor:
+        """The list's workspace on a stream.  What is captured into a graph gets one of its own."""
+        if torch.cuda.is_current_stream_capturing():
+            return torch.empty(self._workspace_bytes, dtype=torch.uint8, device=self.device)
+        ws = self._workspaces.get(stream)
+        if ws is None:
+            ws = self._workspaces.setdefault(stream, torch.zeros(self._workspace_bytes, dtype=torch.uint8, device=self.device))
+        return ws
 
-    def _results(self, buf: torch.Tensor, per_tensor: bool):
-        if per_tensor:
-            return buf.split(self._lengths[1])[1:]
-        return buf[self._norm_at // 4:]
+    def _norms(self, per_tensor: bool) -> torch.Tensor:
+        return torch.empty(1 + len(self.sizes) if per_tensor else 1, dtype=torch.float32, device=self.device)
 
 
 def _disjoint(spans) -> bool:
@@ -522,13 +525,14 @@ def _norm_type(p) -> int:
 def solo_grad_norm(gs: GradSet, norm_type=2, scale: float = 1.0, per_tensor: bool = False):
     """|scale| times the norm (1, 2 or infinity) of the whole list, as a float32 CUDA tensor of one element; with
     `per_tensor` also one of every tensor's norm.  On the current stream, without waiting, as all of these calls."""
-    buf = gs._buffer(per_tensor)
-    base = buf.data_ptr()
-    norm = base + gs._norm_at
-    rc = (_lib or lib()).solo_grad_norm(gs._ref, _norm_type(norm_type), scale, norm, norm + 4 if per_tensor else None, base, _stream())
+    p, stream = _norm_type(norm_type), _stream()
+    out = gs._norms(per_tensor)
+    at = out.data_ptr()
+    with gs._turn:
+        rc = (_lib or lib()).solo_grad_norm(gs._ref, p, scale, at, at + 4 if per_tensor else None, gs._workspace(stream).data_ptr(), stream)
     if rc:
         _check(rc, "solo_grad_norm")
-    return gs._results(buf, per_tensor)
+    return (out[:1], out[1:]) if per_tensor else out
 
 
 def solo_grad_clip(src: GradSet, norms, max_norm: float, dst: GradSet = None, norm_type=2, scale: float = 1.0) -> None:
@@ -550,14 +554,15 @@ def solo_grad_clip(src: GradSet, norms, max_norm: float, dst: GradSet = None, no
 def solo_grad_clip_norm(src: GradSet, max_norm: float, dst: GradSet = None, norm_type=2, scale: float = 1.0,
                         per_tensor: bool = False):
     """solo_grad_norm, and solo_grad_clip by its result, in one call; returns what solo_grad_norm does."""
-    buf = src._buffer(per_tensor)
-    base = buf.data_ptr()
-    norm = base + src._norm_at
-    rc = (_lib or lib()).solo_grad_clip_norm(src._ref, _written(dst or src, src), _norm_type(norm_type), max_norm, scale, norm,
-                                             norm + 4 if per_tensor else None, base, _stream())
+    p, stream, to = _norm_type(norm_type), _stream(), _written(dst or src, src)
+    out = src._norms(per_tensor)
+    at = out.data_ptr()
+    with src._turn:
+        rc = (_lib or lib()).solo_grad_clip_norm(src._ref, to, p, max_norm, scale, at, at + 4 if per_tensor else None,
+                                                 src._workspace(stream).data_ptr(), stream)
     if rc:
         _check(rc, "solo_grad_clip_norm")
-    return src._results(buf, per_tensor)
+    return (out[:1], out[1:]) if per_tensor else out
 
 
 def solo_grad_accumulate(acc: GradSet, grads: GradSet, scale: float = 1.0, first: bool = False, norm_type=None,
@@ -569,14 +574,15 @@ def solo_grad_accumulate(acc: GradSet, grads: GradSet, scale: float = 1.0, first
         if rc:
             _check(rc, "solo_grad_accumulate")
         return None
-    buf = acc._buffer(per_tensor)
-    base = buf.data_ptr()
-    norm = base + acc._norm_at
-    rc = (_lib or lib()).solo_grad_accumulate(_written(acc, grads), grads._ref, scale, 1 if first else 0, _norm_type(norm_type), norm,
-                                              norm + 4 if per_tensor else None, base, _stream())
+    p, stream, to = _norm_type(norm_type), _stream(), _written(acc, grads)
+    out = acc._norms(per_tensor)
+    at = out.data_ptr()
+    with acc._turn:
+        rc = (_lib or lib()).solo_grad_accumulate(to, grads._ref, scale, 1 if first else 0, p, at, at + 4 if per_tensor else None,
+                                                  acc._workspace(stream).data_ptr(), stream)
     if rc:
         _check(rc, "solo_grad_accumulate")
-    return acc._results(buf, per_tensor)
+    return (out[:1], out[1:]) if per_tensor else out
 
 
 _TOKEN_BYTES = {torch.int32: 4, torch.int64: 8}

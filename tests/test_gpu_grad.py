@@ -307,6 +307,42 @@ def test_on_another_stream_and_in_graphs():
         near(d.flat(), s.flat() * min(1.0, 0.125 * (k + 1) / (N + 1e-6)), 12 * U, 2.0 ** -150)
 
 
+def test_threads_take_turns():
+    """Several threads on one stream and several streams of one list: the last CTA's count and the second launches keep apart."""
+    import threading
+    B = lib()
+    sizes = (TILE * 30 + 5, 9, 700) * 8
+    s = Slab(sizes, torch.float16).random(41)
+    gs = B.GradSet(s.views)
+    want = {p: norm64(s.flat(), p) for p in (1, 2, math.inf)}
+    each = {p: torch.tensor([norm64(v, p) for v in s.views], device="cuda", dtype=torch.float64) for p in want}
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    results, errors = [], []
+
+    def work(k):
+        try:
+            with torch.cuda.stream(streams[k % 2]):
+                for i in range(60):
+                    p = (1, 2, math.inf)[(k + i) % 3]
+                    per = (k + i) % 2 == 0
+                    results.append((p, per, B.solo_grad_norm(gs, norm_type=p, per_tensor=per)))
+        except Exception as e:                                            # noqa: BLE001
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not errors and len(results) == 240
+    for p, per, r in results:
+        near_number(r[0] if per else r, want[p], NORM_TOL[p])
+        if per:
+            near(r[1], each[p], NORM_TOL[p])
+
+
 def test_an_accumulator_as_its_own_gradient_and_lists_made_while_capturing():
     B = lib()
     x = torch.randn(3 * TILE + 11, device="cuda")
@@ -395,7 +431,7 @@ def test_refusals():
         B.GradSet([torch.ones(4, 4, device="cuda")[:, 0]])
     with pytest.raises(ValueError):
         B.GradSet([torch.ones(4, device="cuda", dtype=torch.int32)])
-    ws = torch.empty(a._norm_at // 4 + 8, device="cuda")
+    ws = torch.zeros(a._workspace_bytes // 4 + 8, device="cuda")
     out = torch.zeros(1, device="cuda")
     L, p = B.lib(), B.C.byref(a.desc)
     assert L.solo_grad_norm(p, 2, 1.0, out.data_ptr(), None, ws.data_ptr() + 4, None) == B.SOLO_EALIGN
