@@ -36,7 +36,7 @@ constexpr int GU = 4;                      // vectors per thread and tile
 constexpr int GTILE = GCTA * GV * GU;      // elements per tile
 constexpr int GCTAS_PER_SM = 8;            // most CTAs per SM that a launch takes (bounds the workspace)
 constexpr int GFINISH_MOST = 16;           // tensors whose norms the last CTA of a pass finishes too
-constexpr int GIN_FLIGHT = 65536;          // bytes of reads per SM that the resident CTAs of a writing pass have under way (pass())
+constexpr int GIN_FLIGHT = 98304;          // bytes read and written of the tiles that a writing pass has under way per SM (pass())
 
 enum { OP_NORM = 0, OP_CLIP = 1, OP_ACC = 2, OP_ACC_FIRST = 3 };
 
@@ -618,13 +618,13 @@ int pass(int op, const solo_grad_list_t* src, const solo_grad_list_t* dst, int n
     a.tile_start = g->geom + g->num_tensors;
     a.tiles = g->tiles;
     a.num_tensors = g->num_tensors;
-    // Passes that write run best with no more reads under way than it takes (us with 2, 3, 4, 5, 6 CTAs per SM: accumulation of
-    // 809M bf16 1235, 1288, 1287, 1290, 1300; clip of 125M bf16 in place 92, 81, 79, 93, 94; of 809M fp32 to bf16 768, 786,
-    // 784, 761, 761); a pass that only reads takes all that fit (1903 us for 7B bf16 with 4, 1813 with 5).
+    // Passes that write run best with no more under way than it takes: three CTAs per SM for 16-bit gradients in place (GB/s with two and three,
+    // 5720 and 6280; 5850 with four or more), two for the others (201M bf16 into fp32 6110 with two, 5660 with three or more; accumulation of
+    // 809M bf16 1235 us with two, 1290 with three to six).  A pass that only reads takes all that fit (7B bf16: 1903 us with four, 1813 with five).
     int most = per_sm;
     if (op != OP_NORM) {
-        const int per_elem = (src->dtype == SOLO_DT_F32 ? 4 : 2) + (op == OP_ACC ? 4 : 0);
-        most = std::min(per_sm, std::max(2, GIN_FLIGHT / (GTILE * per_elem)));
+        const int written = dst->dtype == SOLO_DT_F32 ? 4 : 2, read = (src->dtype == SOLO_DT_F32 ? 4 : 2) + (op == OP_ACC ? 4 : 0);
+        most = std::min(per_sm, std::max(2, GIN_FLIGHT / (GTILE * (read + written))));
     }
     const int64_t grid = std::max<int64_t>(1, std::min<int64_t>(g->tiles, (int64_t)sm_count(g->device) * most));
     if (grid_out) *grid_out = (int)grid;
