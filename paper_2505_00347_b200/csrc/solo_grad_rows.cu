@@ -349,7 +349,7 @@ template <int RV> struct SumShared {
     uint32_t job_tok[2];
 };
 
-template <int DT, bool VEC, int RV> __global__ __launch_bounds__(ROWS_CTA, 4) void rows_sum_kernel(const __grid_constant__ RowsArgs a) {
+template <int DT, bool VEC, int RV> __global__ __launch_bounds__(ROWS_CTA, VEC ? 4 : 3) void rows_sum_kernel(const __grid_constant__ RowsArgs a) {
     constexpr int SLAB = 32 * RV;
     constexpr uint32_t ALL = 0xFFFFFFFFu, NONE = 0xFFFFFFFFu;
     __shared__ SumShared<RV> s;
@@ -391,7 +391,8 @@ template <int DT, bool VEC, int RV> __global__ __launch_bounds__(ROWS_CTA, 4) vo
     if (lane == 0) s.head[warp] = continues ? (through ? 2 : 1) : 0;
     float sum[RV] = {};
     // Entries whose loads are under way together, few enough for four CTAs per SM (eight columns per lane, 16,384 tokens of 4096
-    // columns: 2 in four CTAs 72.8 us, 4 in three 74.6, 4 in two 84, 8 in two 80).
+    // columns: 2 in four CTAs 72.8 us, 4 in three 74.6, 4 in two 84, 8 in two 80), or three without wide accesses (4098 columns: 91 us, with
+    // four CTAs 102, with two 109).
     constexpr int BATCH = RV == WIDE ? 2 : 4;
     constexpr int ES = DT == SOLO_DT_F32 ? 4 : 2;
     if (lane < count) s.entry[warp][lane] = {(const char*)a.grad + pos * a.grad_stride * ES, a.acc + (int64_t)tok * a.width};
@@ -511,7 +512,7 @@ struct DirectArgs {
     float scale;
 };
 
-template <int DT, bool VEC> __global__ __launch_bounds__(ROWS_CTA) void rows_direct_kernel(const __grid_constant__ DirectArgs a) {
+template <int DT, bool VEC> __global__ __launch_bounds__(ROWS_CTA, 4) void rows_direct_kernel(const __grid_constant__ DirectArgs a) {
     constexpr int RV = WIDE, SLAB = 32 * RV, ES = DT == SOLO_DT_F32 ? 4 : 2;
     constexpr uint32_t ALL = 0xFFFFFFFFu;
     __shared__ float part[ROWS_WARPS][RV][32];
@@ -545,7 +546,8 @@ template <int DT, bool VEC> __global__ __launch_bounds__(ROWS_CTA) void rows_dir
     float old[RV] = {};
     if (alone) cols.load_f32(row, old);
     float total[RV] = {};
-    constexpr int BATCH = 4;
+    // (with registers for four CTAs per SM: 1000 tokens of 770 columns 10.0 us, with four rows and what they take 14.3)
+    constexpr int BATCH = VEC ? 4 : 2;
 #pragma unroll
     for (int k = 0; k < DIRECT_WORDS; ++k) {
         float sum[RV] = {};
