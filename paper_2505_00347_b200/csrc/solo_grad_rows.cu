@@ -78,17 +78,22 @@ template <int ROUNDS, int BITS> __global__ __launch_bounds__(SORT_CTA) void rows
     const int count = min(max(a.num_tokens - first, 0), per_cta);
     const int rounds = (per_cta + SORT_CTA - 1) / SORT_CTA;
     const uint32_t digits = 1u << a.digit_bits;
-    // A warp's tokens follow one another; first from global memory, then from this CTA's places.
+    // A warp's tokens follow one another; first from global memory, then from this CTA's places.  (Without conditions, so that the
+    // loads are under way together: places without a token read the last one.)
     uint2 item[ROUNDS];
     uint32_t rank[ROUNDS];
+    int64_t token[ROUNDS];
+    const auto from = [&](int r) { return min(first + (warp * rounds + min(r, rounds - 1)) * 32 + lane, a.num_tokens - 1); };
+    if (a.token_bytes == 8) {
 #pragma unroll
-    for (int r = 0; r < ROUNDS; ++r) {
-        const int j = (warp * rounds + r) * 32 + lane;
-        if (r < rounds && j < count) {
-            const int64_t t = a.token_bytes == 8 ? ((const int64_t*)a.tokens)[first + j] : (int64_t)((const int32_t*)a.tokens)[first + j];
-            item[r] = make_uint2(t >= 0 && t < a.num_rows ? (uint32_t)t : (uint32_t)a.num_rows, (uint32_t)(first + j));
-        }
+        for (int r = 0; r < ROUNDS; ++r) token[r] = ((const int64_t*)a.tokens)[from(r)];
+    } else {
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) token[r] = ((const int32_t*)a.tokens)[from(r)];
     }
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r)
+        item[r] = make_uint2(token[r] >= 0 && token[r] < a.num_rows ? (uint32_t)token[r] : (uint32_t)a.num_rows, (uint32_t)(first + (warp * rounds + r) * 32 + lane));
     for (int i = me * SORT_CTA + tid; i < a.num_counters; i += ctas * SORT_CTA) a.counters[i] = 0;
     cluster.barrier_wait();
     for (int p = 0; p < a.passes; ++p) {
@@ -181,8 +186,7 @@ template <int ROUNDS, int BITS> __global__ __launch_bounds__(SORT_CTA) void rows
         cluster.sync();
 #pragma unroll
         for (int r = 0; r < ROUNDS; ++r) {
-            const int j = (warp * rounds + r) * 32 + lane;
-            if (r < rounds && j < count) item[r] = s.item[to_buf][j];
+            item[r] = s.item[to_buf][min((warp * rounds + r) * 32 + lane, SORT_PER_CTA - 1)];
         }
     }
 #pragma unroll
