@@ -2,7 +2,7 @@
 //
 // Two launches for up to 65,536 tokens.  A cluster of up to sixteen CTAs sorts the tokens with their positions in its shared memory
 // (least significant digit first, stable, so that equal tokens keep their order); then a CTA takes 128 entries of the sorted
-// order and 256 columns, a warp 16 of these entries.  A warp sums the rows of each run of equal tokens in registers; runs that
+// order and 256 or 128 columns, a warp 16 of these entries.  A warp sums the rows of each run of equal tokens in registers; runs that
 // lie in one warp's entries are added to the accumulator at once, the pieces of others are put together in shared memory, and those of
 // runs that reach into other CTAs in the workspace, by the CTA that finishes last, in their order.  So every row of the
 // accumulator is read and written once, without atomics and in an order that the tokens alone decide, and a CTA has the
@@ -40,6 +40,7 @@ constexpr int DIGIT_MAX = 9, DIGITS = 1 << DIGIT_MAX;
 constexpr int ROWS_WARPS = 8, ROWS_CTA = ROWS_WARPS * 32;   // of the summing kernel
 constexpr int WARP_ROWS = 16, CTA_ROWS = ROWS_WARPS * WARP_ROWS;
 constexpr int REACH = 8;                               // entries of the next CTA that a run's end may take up and stay whole
+constexpr double AHEAD = 48e6;                         // bytes brought to L2 while the sort runs, at most
 constexpr int WIDE = 8, NARROW = 4;                    // columns of a lane; a CTA has 32 times as many
 
 struct SortArgs {
@@ -209,6 +210,9 @@ struct RowsArgs {
     int64_t width, grad_stride;
     int32_t num_tokens, num_rows, slabs;
     float scale;
+    // what is brought to L2 while the sort runs: rows of gradients, and with `tokens` (the unsorted ones) of the accumulator
+    const void* tokens;
+    int32_t token_bytes, ahead_ctas, ahead_rows;
 };
 
 // Loads that are issued where they are written, so that those of several rows are under way together: a compiler may move a
@@ -341,6 +345,27 @@ template <class Border> __device__ __forceinline__ int ctas_reached(uint32_t fir
     }
 }
 
+// The CTAs of the sum that are resident while the sort runs have nothing else to do: they bring rows to L2 (16,384 tokens of 768 columns 34.8 ->
+// 32.8 us with nothing in L2 before, 24.5 -> 23.7 us call after call).  Nothing of it is needed, and the tokens read here, before the wait
+// for the kernels before, choose addresses in the table and nothing else.
+template <int DT> __device__ __forceinline__ void rows_ahead(const RowsArgs& a) {
+    constexpr int LINE = 128, ES = DT == SOLO_DT_F32 ? 4 : 2;
+    const int threads = a.ahead_ctas * ROWS_CTA, me = blockIdx.x * ROWS_CTA + threadIdx.x;
+    const int lines = (int)((a.width * ES + LINE - 1) / LINE);
+    for (int64_t i = me; i < (int64_t)a.ahead_rows * lines; i += threads) {
+        const char* const p = (const char*)a.grad + (i / lines) * a.grad_stride * ES + (i % lines) * LINE;
+        asm volatile("prefetch.global.L2 [%0];" :: "l"(p));
+    }
+    if (!a.tokens) return;
+    const int acc_lines = (int)((a.width * 4 + LINE - 1) / LINE);
+    for (int64_t i = me; i < (int64_t)a.num_tokens * acc_lines; i += threads) {
+        const int64_t t = a.token_bytes == 8 ? __ldcg((const long long*)a.tokens + i / acc_lines) : (int64_t)__ldcg((const int*)a.tokens + i / acc_lines);
+        if (t < 0 || t >= a.num_rows) continue;
+        const char* const p = (const char*)(a.acc + t * a.width) + (i % acc_lines) * LINE;
+        asm volatile("prefetch.global.L2 [%0];" :: "l"(p));
+    }
+}
+
 template <int RV> struct SumShared {
     union {
         float open[2][ROWS_WARPS][RV][32];       // pieces of runs that a warp does not hold whole: what continues one, what begins one
@@ -357,6 +382,7 @@ template <int DT, bool VEC, int RV> __global__ __launch_bounds__(ROWS_CTA, VEC ?
     constexpr int SLAB = 32 * RV;
     constexpr uint32_t ALL = 0xFFFFFFFFu, NONE = 0xFFFFFFFFu;
     __shared__ SumShared<RV> s;
+    if (blockIdx.x < (unsigned)a.ahead_ctas) rows_ahead<DT>(a);
     pdl_wait();
     pdl_release();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -771,6 +797,13 @@ int solo_grad_accumulate_rows(const solo_grad_rows_t* r, float scale, void* work
         a.num_rows = s.num_rows;
         a.slabs = (int32_t)slabs;
         a.scale = scale;
+        const double row_bytes = (double)r->width * es, all = n * row_bytes, acc_all = (double)n * (double)r->width * 4;
+        a.ahead_ctas = (int32_t)std::min<int64_t>(row_ctas, (vec ? 4 : 3) * sm_count(device));
+        a.ahead_rows = (int32_t)std::min<double>(n, AHEAD / row_bytes);
+        if (all + acc_all <= AHEAD) {
+            a.tokens = s.tokens;
+            a.token_bytes = s.token_bytes;
+        }
         void* rp[] = {&a};
         rc = launch((const void*)rows_kernel_for(r->grad_dtype, vec, rv), dim3((unsigned)row_ctas), ROWS_CTA, 0, 0, rp, stream);
         if (rc != SOLO_OK) return rc;
