@@ -16,7 +16,7 @@
  *   - Functions return SOLO_OK (0) or a negative solo_status_t.  Nothing throws,
  *     aborts or traps on the device.  Arguments are validated on the host before
  *     anything is launched; a rejected call has no effect.
- *   - Gradients are bf16.  Parameters are fp32 or bf16 and are updated in place.
+ *   - The step's gradients are bf16.  Parameters are fp32 or bf16 and are updated in place.
  *   - bits is 2, 3, 4 or 8 independently for the two moments; block is 64, 128,
  *     256 or 2048 elements.
  *
@@ -45,7 +45,7 @@ extern "C" {
 typedef enum {
     SOLO_OK = 0,
     SOLO_EINVAL = -1,   /* bad argument value (bits, block, numel, null pointer, ...) */
-    SOLO_EALIGN = -2,   /* a parameter / gradient pointer is not 16-byte aligned */
+    SOLO_EALIGN = -2,   /* a parameter / gradient pointer is not 16-byte aligned, or another one not as its call says */
     SOLO_ENOMEM = -3,   /* device or host allocation failed */
     SOLO_ECUDA = -4,    /* a CUDA runtime call or the kernel launch failed */
     SOLO_ESTATE = -5,   /* the state does not match the call (sizes, tensor count) */
@@ -400,7 +400,8 @@ int solo_static_status(int* status_out, void* stream);
  *   solo_multi_step on the bf16 gradients
  *
  * Sums are taken in binary32 over at most 32 elements of a thread and in binary64 from there on, in
- * an order that depends on the tensor sizes and the device only: the same inputs give the same bits.
+ * an order that depends on the tensors' sizes and alignment, the device and whether every tensor's norm is asked for,
+ * and on nothing else: the same call on the same inputs gives the same bits.
  * Squares that binary32 cannot hold (overflow, underflow) are summed in binary64.
  */
 enum { SOLO_DT_F32 = 0, SOLO_DT_BF16 = 1, SOLO_DT_F16 = 2 };       /* element types of a gradient list */
@@ -420,8 +421,8 @@ int solo_grads_create(const int64_t* numel_host, int num_tensors, int64_t* geom_
 /* Frees the handle's host memory.  NULL is accepted. */
 int solo_grads_destroy(solo_grads_t* grads);
 /* Bytes of the workspace that the calls with a norm need (16-byte aligned device memory).  Its first 16 bytes are zero before
- * its first use, and every call leaves them so; the rest may hold anything, and in a call that is captured all of it.  Calls that may run at the same time need one
- * each; so do threads that call on one stream without taking turns. */
+ * its first use, and every call leaves them so; the rest may hold anything, and in a call that is captured all of it.
+ * Calls that may run at the same time need one each; so do threads that call on one stream without taking turns. */
 int solo_grads_workspace(const solo_grads_t* grads, size_t* bytes);
 
 /*
@@ -475,7 +476,7 @@ int solo_grad_accumulate(const solo_grad_list_t* acc, const solo_grad_list_t* gr
  * Tokens outside [0, num_rows) (padding, masked positions) contribute nothing, whatever their rows hold; rows of acc that no
  * token names stay as they are.  The rows of one token are summed in binary32 in groups (fewer than 48 additions follow one another) and
  * the groups in binary64, for 65,536 tokens together; each such sum is added with one rounding.  The order depends on the
- * tokens alone: the same inputs give the same bits.
+ * tokens and their number, and on the width: the same inputs give the same bits.
  */
 typedef struct {
     float* acc;                  /* device [num_rows, width], binary32 */
