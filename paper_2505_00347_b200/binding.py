@@ -464,7 +464,7 @@ class GradSet:
         _check(lib().solo_grads_workspace(self.handle, C.byref(n)), "solo_grads_workspace")
         self.desc = GradList(self.handle.value, self.ptrs.data_ptr(), _GRAD_DTYPE[dtype])
         self._ref = C.byref(self.desc)
-        self._workspace_bytes = n.value
+        self._workspace_bytes, self._lengths = n.value, [1, len(grads)]
         self._workspaces = {}         # by stream: calls on one stream follow one another
         self._turn = threading.Lock()
 
@@ -532,7 +532,7 @@ def solo_grad_norm(gs: GradSet, norm_type=2, scale: float = 1.0, per_tensor: boo
         rc = (_lib or lib()).solo_grad_norm(gs._ref, p, scale, at, at + 4 if per_tensor else None, gs._workspace(stream).data_ptr(), stream)
     if rc:
         _check(rc, "solo_grad_norm")
-    return (out[:1], out[1:]) if per_tensor else out
+    return out.split_with_sizes(gs._lengths) if per_tensor else out
 
 
 def solo_grad_clip(src: GradSet, norms, max_norm: float, dst: GradSet = None, norm_type=2, scale: float = 1.0) -> None:
@@ -562,7 +562,7 @@ def solo_grad_clip_norm(src: GradSet, max_norm: float, dst: GradSet = None, norm
                                                  src._workspace(stream).data_ptr(), stream)
     if rc:
         _check(rc, "solo_grad_clip_norm")
-    return (out[:1], out[1:]) if per_tensor else out
+    return out.split_with_sizes(src._lengths) if per_tensor else out
 
 
 def solo_grad_accumulate(acc: GradSet, grads: GradSet, scale: float = 1.0, first: bool = False, norm_type=None,
@@ -582,7 +582,7 @@ def solo_grad_accumulate(acc: GradSet, grads: GradSet, scale: float = 1.0, first
                                                   acc._workspace(stream).data_ptr(), stream)
     if rc:
         _check(rc, "solo_grad_accumulate")
-    return (out[:1], out[1:]) if per_tensor else out
+    return out.split_with_sizes(acc._lengths) if per_tensor else out
 
 
 _TOKEN_BYTES = {torch.int32: 4, torch.int64: 8}
