@@ -449,7 +449,7 @@ int solo_grad_norm(const solo_grad_list_t* list, int norm_type, float scale, flo
  * together from `norms_dev`, a device array of `num_norms` floats, as the norm of the whole of which
  * these are the norms of the parts (the workers' shards; one value where there are none); they are
  * norms of the scaled gradients, as solo_grad_norm gives them.  num_norms = 0: f = scale, a plain
- * scaling or conversion.  `dst` may be `src` (in place; nothing is read or written then if f is 1) or
+ * scaling or conversion.  `dst` may be `src` (in place; if f is 1 nothing is written then and next to nothing read) or
  * a list of the same sizes and any type.  A norm that is NaN makes everything NaN, an infinite one
  * finite gradients 0; max_norm is finite and not negative.  No tensor of `dst` overlaps another one.
  */

@@ -356,6 +356,12 @@ template <int OP, int DS, int DD, int NT> __global__ __launch_bounds__(GCTA, OP 
     Place<DS, DD, WRITES> at;
     if (x < end) at.start(a, tile(x));
     while (x < end) {
+        if (OP == OP_CLIP && DS == DD && have_f && f == 1.0f && (const char*)at.d == at.s) {        // in place, by one: nothing changes
+            if ((const void*)a.src == (const void*)a.dst) break;                // in none of the tensors
+            x += step;
+            if (x < end) at.move(a, tile(x));
+            continue;
+        }
         const int64_t off = tile(x) - at.t0, base = at.head + off * GTILE;
         const bool full = at.vec && base + GTILE <= at.n;
         const int64_t first = off == 0 ? 0 : base;
@@ -388,7 +394,7 @@ template <int OP, int DS, int DD, int NT> __global__ __launch_bounds__(GCTA, OP 
             x += step;
             if (x < end) at.move(a, tile(x));
         }
-        if (OP == OP_CLIP && DS == DD && f == 1.0f && same) continue;           // in place, by one: nothing changes
+        if (OP == OP_CLIP && DS == DD && f == 1.0f && same) continue;           // (the tile that was loaded before the factor was known)
         if (full) {
 #pragma unroll
             for (int u = 0; u < GU; ++u) {
