@@ -1,7 +1,8 @@
 // The gradient of an embedding, added to its fp32 accumulator: acc[tok_i, :] += s * g[i, :] (include/solo.h).
 //
-// Two launches for up to 65,536 tokens.  A cluster of up to sixteen CTAs sorts the tokens with their positions in its shared memory
-// (least significant digit first, stable, so that equal tokens keep their order); then a CTA takes 128 entries of the sorted
+// Two launches for up to 65,536 tokens.  The first puts the tokens and their positions in order, equal tokens in the order they came in: up
+// to RANK_MOST of them by counting, for every token, those that come before it; more in the shared memory of a cluster of up to sixteen
+// CTAs, least significant digit first.  Then a CTA takes 128 entries of the sorted
 // order and 256 or 128 columns, a warp 16 of these entries.  A warp sums the rows of each run of equal tokens in registers; runs that
 // lie in one warp's entries are added to the accumulator at once, the pieces of others are put together in shared memory, and those of
 // runs that reach into other CTAs in the workspace, by the CTA that finishes last, in their order.  So every row of the
@@ -200,6 +201,63 @@ template <int ROUNDS, int BITS> __global__ __launch_bounds__(SORT_CTA) void rows
     }
 }
 
+// Two sums in one instruction.
+__device__ __forceinline__ void add_pair(float& a, float& b, float x, float y) {
+    asm("{ .reg .b64 s, t; mov.b64 s, {%0, %1}; mov.b64 t, {%2, %3}; add.rn.f32x2 s, s, t; mov.b64 {%0, %1}, s; }" : "+f"(a), "+f"(b) : "f"(x), "f"(y));
+}
+
+// The place of every token is the number of tokens that are smaller, or equal and before it: a lane per token, an eighth of the tokens
+// per warp.  n^2 comparisons, but no step that waits for another CTA (rank_first() has the times of both).  A comparison is the
+// saturation of a difference of whole numbers, exactly 0 or 1, on the pipe for fp32, which takes a warp every cycle where integer
+// comparisons take one every other.
+constexpr int RANK_MOST = 4096, RANK_ROWS = (1 << 24) - 2;
+
+__global__ __launch_bounds__(SORT_CTA) void rows_rank_kernel(const __grid_constant__ SortArgs a) {
+    __shared__ __align__(16) float key[RANK_MOST];
+    __shared__ float part[SORT_WARPS][32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = a.num_tokens;
+    pdl_wait();
+    pdl_release();
+    const int quads = (n + 3) / 4;
+    const auto load = [&](auto tokens) {
+#pragma unroll 8
+        for (int j = tid; j < 4 * quads; j += SORT_CTA) {
+            const int64_t t = tokens[min(j, n - 1)];
+            key[j] = j >= n ? __int_as_float(0x7F800000) : (float)(t >= 0 && t < a.num_rows ? (int)t : a.num_rows);
+        }
+    };
+    if (a.token_bytes == 8) load((const int64_t*)a.tokens);
+    else load((const int32_t*)a.tokens);
+    for (int i = blockIdx.x * SORT_CTA + tid; i < a.num_counters; i += gridDim.x * SORT_CTA) a.counters[i] = 0;
+    __syncthreads();
+    const int i0 = blockIdx.x * 32, i = i0 + lane;
+    const float t = key[min(i, n - 1)];
+    const int lo = quads * warp / SORT_WARPS, hi = quads * (warp + 1) / SORT_WARPS;         // in quads, as this CTA's own tokens: q0 to q0 + 7
+    const int q0 = i0 / 4;
+    const float4* const quad = reinterpret_cast<const float4*>(key);
+    float before[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    const auto count = [&](int from, int to, float limit) {
+#pragma unroll 8
+        for (int q = from; q < to; ++q) {
+            const float4 k = quad[q];
+            add_pair(before[0], before[1], __saturatef(limit - k.x), __saturatef(limit - k.y));
+            add_pair(before[2], before[3], __saturatef(limit - k.z), __saturatef(limit - k.w));
+        }
+    };
+    count(lo, min(hi, q0), t + 1.0f);
+    for (int j = 4 * max(lo, q0); j < 4 * min(hi, q0 + 8); ++j) before[0] += __saturatef(t + (j < i ? 1.0f : 0.0f) - key[j]);
+    count(max(lo, q0 + 8), hi, t);
+    part[warp][lane] = (before[0] + before[1]) + (before[2] + before[3]);
+    __syncthreads();
+    if (warp == 0 && i < n) {
+        float place = 0.0f;
+#pragma unroll
+        for (int w = 0; w < SORT_WARPS; ++w) place += part[w][lane];
+        a.tok[(int)place] = (uint32_t)t;
+        a.pos[(int)place] = (uint16_t)i;
+    }
+}
+
 struct RowsArgs {
     float* acc;
     const void* grad;
@@ -246,10 +304,6 @@ template <int DT> __device__ __forceinline__ float row_elem(const char* g, int64
         if constexpr (DT == SOLO_DT_BF16) return __uint_as_float((uint32_t)h << 16);
         else return __half2float(__ushort_as_half(h));
     }
-}
-// Two sums in one instruction.
-__device__ __forceinline__ void add_pair(float& a, float& b, float x, float y) {
-    asm("{ .reg .b64 s, t; mov.b64 s, {%0, %1}; mov.b64 t, {%2, %3}; add.rn.f32x2 s, s, t; mov.b64 {%0, %1}, s; }" : "+f"(a), "+f"(b) : "f"(x), "f"(y));
 }
 
 // RV columns of a thread: consecutive ones and wide accesses (VEC), or one in every 32.  A thread without columns of its own reads
@@ -667,7 +721,7 @@ SortKernel sort_kernel_for(int rounds, int bits) {
     return bits <= 8 ? rows_sort_kernel<SORT_PER_CTA / SORT_CTA, 8> : rows_sort_kernel<SORT_PER_CTA / SORT_CTA, DIGIT_MAX>;
 }
 
-// The sort's shared memory and clusters of sixteen, opted in to once per device.
+// Shared memory and clusters of sixteen, opted in to once per device.
 int sort_ready(int& device) {
     static std::atomic<bool> done[64];
     device = -1;
@@ -682,9 +736,17 @@ int sort_ready(int& device) {
                 return SOLO_ECUDA;
             }
         }
+    // As much shared memory as the sum's CTAs ask for: an SM has to run empty before it is divided another way (3000 tokens of 4096
+    // columns 20.3 us, without this 24.7).
+    if (cudaFuncSetAttribute((const void*)rows_rank_kernel, cudaFuncAttributePreferredSharedMemoryCarveout, 30) != cudaSuccess) cudaGetLastError();
     done[device] = true;
     return SOLO_OK;
 }
+
+// Whether the order of a chunk comes from counting or from the sort.  Us with the sum, counting and sorting: 2048 tokens of 768 columns 9.2 and
+// 11.8, 4096 11.2 and 14.3, 6000 17.4 and 15.7; of 4096 columns 2048 12.5 and 16.0, 3000 20.3 and 21.0, 4096 27.1 and 25.7; 4096
+// of 2000 columns 16.0 and 17.2.
+bool rank_first(int n, int64_t num_rows, int64_t width) { return n <= (width <= 2048 ? RANK_MOST : 2048) && num_rows <= RANK_ROWS; }
 
 struct RowsLayout { size_t tok, pos, counters, partial, total; };
 
@@ -781,7 +843,8 @@ int solo_grad_accumulate_rows(const solo_grad_rows_t* r, float scale, void* work
         while (ctas < SORT_CLUSTER && n > ctas * SORT_AIM) ctas *= 2;
         while ((ctas << s.log_per_cta) < n) ++s.log_per_cta;
         void* sp[] = {&s};
-        rc = launch((const void*)sort_kernel_for((1 << s.log_per_cta) / SORT_CTA, s.digit_bits), dim3((unsigned)ctas), SORT_CTA, sizeof(SortShared), ctas, sp, stream);
+        if (rank_first(n, r->num_rows, r->width)) rc = launch((const void*)rows_rank_kernel, dim3((unsigned)((n + 31) / 32)), SORT_CTA, 0, 0, sp, stream);
+        else rc = launch((const void*)sort_kernel_for((1 << s.log_per_cta) / SORT_CTA, s.digit_bits), dim3((unsigned)ctas), SORT_CTA, sizeof(SortShared), ctas, sp, stream);
         if (rc != SOLO_OK) return rc;
         RowsArgs a;
         std::memset(&a, 0, sizeof(a));

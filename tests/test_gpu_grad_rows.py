@@ -60,7 +60,7 @@ def check(acc, tok, grad, scale, **kw):
 
 
 @pytest.mark.parametrize("kind", ["same", "distinct", "sorted", "outside", "few", "skewed"])
-@pytest.mark.parametrize("n", [1, 2, 31, 33, 63, 64, 65, 95, 96, 97, 128, 161, 1000, 2048, 2049, 5000, 16385, 65536])
+@pytest.mark.parametrize("n", [1, 2, 31, 33, 63, 64, 65, 95, 96, 97, 128, 161, 1000, 1025, 2048, 2049, 4093, 4096, 4097, 5000, 16385, 65536])
 def test_token_patterns(kind, n):
     gen = torch.Generator(device="cuda").manual_seed(n)
     for rows, width in ((50257, 16), (1000, 24), (3, 5), (1, 8)):
@@ -127,11 +127,13 @@ def test_more_tokens_than_one_sort_holds():
 
 def test_wide_vocabularies():
     gen = torch.Generator(device="cuda").manual_seed(6)
-    for rows in (255, 256, 511, 512, 513, 65535, 65536, 262143, 262144, 3_000_000):
-        acc = torch.randn(rows, 4, generator=gen, device="cuda")
-        tok = tokens_of("skewed", 4000, rows).cuda()
-        tok[:3] = torch.tensor([rows - 1, rows, 0])
-        check(acc, tok, torch.randn(4000, 4, generator=gen, device="cuda"), 1.0)
+    for rows in (255, 256, 511, 512, 513, 65535, 65536, 262143, 262144, 3_000_000, (1 << 24) - 2, (1 << 24) - 1, (1 << 24) + 5):
+        for n in (1500, 4000, 5000):                    # the order by counting and by the sort
+            acc = torch.randn(rows, 4, generator=gen, device="cuda")
+            tok = tokens_of("skewed", n, rows).cuda()
+            tok[:3] = torch.tensor([rows - 1, rows, 0])
+            tok[3:100] = rows - 1 - torch.arange(97, device="cuda") % min(rows, 50)
+            check(acc, tok, torch.randn(n, 4, generator=gen, device="cuda"), 1.0)
 
 
 def test_values_of_masked_rows_do_not_matter_and_others_come_through():
