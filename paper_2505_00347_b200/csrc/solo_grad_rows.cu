@@ -736,9 +736,15 @@ int sort_ready(int& device) {
                 return SOLO_ECUDA;
             }
         }
-    // As much shared memory as the sum's CTAs ask for: an SM has to run empty before it is divided another way (3000 tokens of 4096
-    // columns 20.3 us, without this 24.7).
-    if (cudaFuncSetAttribute((const void*)rows_rank_kernel, cudaFuncAttributePreferredSharedMemoryCarveout, 30) != cudaSuccess) cudaGetLastError();
+    // How an SM is divided into shared memory and L1.  It has to run empty before it is divided another way, so the counting asks for no more
+    // than the sum (3000 tokens of 4096 columns 20.3 us, left to itself 24.7); the sum asks for what four of its CTAs take and little more
+    // (16,384 tokens of 4096 columns 67.1 us, left to itself 69.5; 30,000 of 1000 columns 51.8 and 58.7).  Wishes: a refusal does not matter.
+    cudaFuncSetAttribute((const void*)rows_rank_kernel, cudaFuncAttributePreferredSharedMemoryCarveout, 30);
+    for (int dtype : {SOLO_DT_F32, SOLO_DT_BF16, SOLO_DT_F16})
+        for (int rv : {NARROW, WIDE})
+            for (bool vec : {false, true})
+                cudaFuncSetAttribute((const void*)rows_kernel_for(dtype, vec, rv), cudaFuncAttributePreferredSharedMemoryCarveout, 45);
+    cudaGetLastError();
     done[device] = true;
     return SOLO_OK;
 }
