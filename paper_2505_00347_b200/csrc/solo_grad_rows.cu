@@ -432,7 +432,9 @@ template <int RV> struct SumShared {
     uint32_t job_tok[2];
 };
 
-template <int DT, bool VEC, int RV> __global__ __launch_bounds__(ROWS_CTA, VEC ? 4 : 3) void rows_sum_kernel(const __grid_constant__ RowsArgs a) {
+template <bool VEC, int RV> constexpr int SUM_CTAS = VEC && RV == WIDE ? 4 : 3;       // per SM
+
+template <int DT, bool VEC, int RV> __global__ __launch_bounds__(ROWS_CTA, SUM_CTAS<VEC, RV>) void rows_sum_kernel(const __grid_constant__ RowsArgs a) {
     constexpr int SLAB = 32 * RV;
     constexpr uint32_t ALL = 0xFFFFFFFFu, NONE = 0xFFFFFFFFu;
     __shared__ SumShared<RV> s;
@@ -475,8 +477,8 @@ template <int DT, bool VEC, int RV> __global__ __launch_bounds__(ROWS_CTA, VEC ?
     if (lane == 0) s.head[warp] = continues ? (through ? 2 : 1) : 0;
     float sum[RV] = {};
     // Entries whose loads are under way together, few enough for four CTAs per SM (eight columns per lane, 16,384 tokens of 4096
-    // columns: 2 in four CTAs 72.8 us, 4 in three 74.6, 4 in two 84, 8 in two 80), or three without wide accesses (4098 columns: 91 us, with
-    // four CTAs 102, with two 109).
+    // columns: 2 in four CTAs 67.1 us, 2 in three 72.1, 4 in three 74.5, 2 in five 79), or three with four columns per lane (768 columns 22.6 us,
+    // in four CTAs 23.7) and without wide accesses (4098 columns 91 us, in four CTAs 102, in two 109).
     constexpr int BATCH = RV == WIDE ? 2 : 4;
     constexpr int ES = DT == SOLO_DT_F32 ? 4 : 2;
     if (lane < count) s.entry[warp][lane] = {(const char*)a.grad + pos * a.grad_stride * ES, a.acc + (int64_t)tok * a.width};
@@ -867,7 +869,7 @@ int solo_grad_accumulate_rows(const solo_grad_rows_t* r, float scale, void* work
         a.slabs = (int32_t)slabs;
         a.scale = scale;
         const double row_bytes = (double)r->width * es, all = n * row_bytes, acc_all = (double)n * (double)r->width * 4;
-        a.ahead_ctas = (int32_t)std::min<int64_t>(row_ctas, (vec ? 4 : 3) * sm_count(device));
+        a.ahead_ctas = (int32_t)std::min<int64_t>(row_ctas, (vec && rv == WIDE ? 4 : 3) * sm_count(device));
         a.ahead_rows = (int32_t)std::min<double>(n, AHEAD / row_bytes);
         if (all + acc_all <= AHEAD) {
             a.tokens = s.tokens;
