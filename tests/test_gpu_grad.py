@@ -307,6 +307,36 @@ def test_on_another_stream_and_in_graphs():
         near(d.flat(), s.flat() * min(1.0, 0.125 * (k + 1) / (N + 1e-6)), 12 * U, 2.0 ** -150)
 
 
+def test_captured_norms_of_every_tensor_and_many_parts():
+    B = lib()
+    for sizes in (RAGGED[:6], LONG):
+        s, acc = Slab(sizes, torch.float16).random(51), Slab(sizes, torch.float32).random(52)
+        gs, al = B.GradSet(s.views), B.GradSet(acc.views)
+        eager = B.solo_grad_norm(gs, per_tensor=True)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            total, per = B.solo_grad_norm(gs, per_tensor=True)
+            after, after_per = B.solo_grad_accumulate(al, gs, scale=0.5, norm_type=1, per_tensor=True)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(total, eager[0]) and torch.equal(per, eager[1])
+        for seed in (53, 54):
+            s.random(seed)
+            graph.replay()
+            torch.cuda.synchronize()
+            near_number(total, norm64(s.flat(), 2), NORM_TOL[2])
+            near(per, torch.tensor([norm64(v, 2) for v in s.views], device="cuda", dtype=torch.float64), NORM_TOL[2])
+            near_number(after, norm64(acc.flat(), 1), NORM_TOL[1])
+            near(after_per, torch.tensor([norm64(v, 1) for v in acc.views], device="cuda", dtype=torch.float64), NORM_TOL[1])
+        assert torch.equal(B.solo_grad_norm(gs, per_tensor=True)[1], per)             # and outside of it again
+    x = torch.ones(TILE + 1, device="cuda")
+    parts = torch.rand(5000, device="cuda")
+    for p in (1, 2, math.inf):
+        y = torch.empty_like(x)
+        B.solo_grad_clip(B.GradSet([x]), parts, 0.25, dst=B.GradSet([y]), norm_type=p)
+        near(y, x.double() * (0.25 / (norm64(parts, p) + 1e-6)), 3 * U)
+
+
 def test_threads_take_turns():
     """Several threads on one stream and several streams of one list: the last CTA's count and the second launches keep apart."""
     import threading
