@@ -485,12 +485,13 @@ typedef struct {
     const void* tokens;          /* device [num_tokens] */
     int32_t token_bytes;         /* 4: int32, 8: int64 */
     int32_t grad_dtype;          /* SOLO_DT_* */
-    const void* grad;            /* device: row i starts grad_stride * i elements after row 0; does not overlap acc */
-    int64_t grad_stride;         /* >= 0 */
+    const void* grad;            /* device: row i starts grad_stride * i elements after row 0 */
+    int64_t grad_stride;         /* >= 0; the rows end within 2^60 elements */
     int64_t num_tokens;          /* 0 .. 2^40 */
 } solo_grad_rows_t;
 /* `workspace_dev`: 16-byte aligned device memory of solo_grad_rows_workspace's size, NULL if that is 0.  It may hold anything; calls
- * that may run at the same time need one each. */
+ * that may run at the same time need one each.  acc and the workspace share no memory with each other, the tokens or grad's rows
+ * (SOLO_EINVAL). */
 int solo_grad_rows_workspace(int64_t num_tokens, int64_t width, size_t* bytes);
 int solo_grad_accumulate_rows(const solo_grad_rows_t* rows, float scale, void* workspace_dev, void* stream);
 

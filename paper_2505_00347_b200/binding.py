@@ -598,7 +598,8 @@ def _rows_workspace(num_tokens: int, width: int) -> int:
 def solo_grad_accumulate_rows(acc: torch.Tensor, tokens: torch.Tensor, grad: torch.Tensor, scale: float = 1.0) -> None:
     """acc[tokens[i], :] += scale * grad[i, :], the gradient of an embedding.  acc: fp32 [rows, width], contiguous; tokens:
     int32 or int64 of any shape, contiguous; grad: fp32, bf16 or fp16 of that shape and a last dimension of width, contiguous
-    or, with one dimension of tokens, with rows any distance apart.  Tokens outside the table contribute nothing."""
+    or, with one dimension of tokens, with rows any distance apart.  Tokens outside the table contribute nothing.  acc shares no
+    memory with tokens or the rows of grad: refused."""
     if acc.dim() != 2 or acc.dtype != torch.float32 or not acc.is_cuda or not acc.is_contiguous():
         raise ValueError("acc must be a contiguous float32 CUDA matrix")
     num_rows, width = acc.shape

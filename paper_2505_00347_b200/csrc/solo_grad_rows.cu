@@ -777,7 +777,17 @@ RowsLayout rows_layout(int64_t num_tokens, int64_t width) {
     return l;
 }
 
-constexpr int64_t MOST_WIDTH = (int64_t)1 << 24, MOST_TOKENS = (int64_t)1 << 40;
+constexpr int64_t MOST_WIDTH = (int64_t)1 << 24, MOST_TOKENS = (int64_t)1 << 40, MOST_ELEMS = (int64_t)1 << 60;
+
+// Whether `bytes` at a share memory with one of n pieces of `piece` bytes, the first at b and one every `step` bytes.
+bool meets(const void* a, size_t bytes, const void* b, int64_t n, size_t piece, size_t step) {
+    const uintptr_t lo = (uintptr_t)a, first = (uintptr_t)b;
+    if (bytes == 0 || (first > lo && first - lo >= bytes)) return false;                // all of them behind
+    if (first > lo || lo - first < piece) return true;
+    if (step == 0) return false;
+    const uint64_t i = (lo - first - piece) / step + 1;                                 // the first one that ends behind lo
+    return i < (uint64_t)n && (first + i * step <= lo || first + i * step - lo < bytes);
+}
 
 }  // namespace
 }  // namespace solo
@@ -803,9 +813,17 @@ int solo_grad_accumulate_rows(const solo_grad_rows_t* r, float scale, void* work
     if (((uintptr_t)workspace_dev & 15u) || ((uintptr_t)r->acc & 3u) || ((uintptr_t)r->tokens & (unsigned)(r->token_bytes - 1)) ||
         ((uintptr_t)r->grad & (unsigned)(es - 1)))
         return SOLO_EALIGN;
+    if (r->grad_stride > MOST_ELEMS || (r->grad_stride && r->num_tokens - 1 > (MOST_ELEMS - r->width) / r->grad_stride)) return SOLO_EINVAL;
+    // What is written, acc and the workspace, lies apart from each other and from what is read.
+    const RowsLayout l = rows_layout(r->num_tokens, r->width);
+    const size_t row = (size_t)r->width * es, acc_bytes = (size_t)r->num_rows * (size_t)r->width * 4, ws_bytes = direct ? 0 : l.total;
+    const auto apart = [&](const void* p, size_t bytes) {
+        return !meets(p, bytes, r->tokens, r->num_tokens, r->token_bytes, r->token_bytes) &&
+               !meets(p, bytes, r->grad, r->num_tokens, row, (size_t)r->grad_stride * es);
+    };
+    if (!apart(r->acc, acc_bytes) || !apart(workspace_dev, ws_bytes) || meets(workspace_dev, ws_bytes, r->acc, 1, acc_bytes, 0)) return SOLO_EINVAL;
     cudaStream_t stream = (cudaStream_t)stream_;
     const bool vec = r->width % WIDE == 0 && (((uintptr_t)r->acc | (uintptr_t)r->grad) & 15u) == 0 && (r->grad_stride * es) % 16 == 0;
-    const RowsLayout l = rows_layout(r->num_tokens, r->width);
     if (direct) {
         DirectArgs d;
         std::memset(&d, 0, sizeof(d));

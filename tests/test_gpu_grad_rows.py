@@ -226,3 +226,41 @@ def test_refusals():
         with pytest.raises(B.SoloError):
             B.solo_grad_accumulate_rows(acc, tok, grad, scale=bad)
     assert float(acc.abs().sum()) == 0.0
+
+
+def test_accumulators_next_to_and_over_what_is_read():
+    """acc, the gradient's rows and the tokens in one buffer: refused where acc shares memory with either, added where it does not."""
+    B = lib()
+    gen = torch.Generator(device="cuda").manual_seed(12)
+    refused = added = 0
+    for n in (3, 1100):
+        for rows, width, stride in ((5, 8, 8), (5, 8, 64), (2, 4, 13), (1, 16, 40), (3, 8, 0)):
+            size, span = rows * width, (n - 1) * stride + width
+            buf = torch.empty(size + span + 2 * size + 2 * n + 64, device="cuda")
+            at = size + 8                                                           # where the gradient starts
+            for acc_at in sorted({0, 8, 9, size, at, at + width - 1, at + width, at + stride, at + 2 * stride - size, at + 2 * stride - size + 1,
+                                  at + span - 1, at + span, at + span + 5}):
+                buf.normal_(generator=gen)
+                tok_at = (at + span + size + 6 + 1) // 2
+                tok = buf.view(torch.int64)[tok_at:tok_at + n] if buf.numel() % 2 == 0 else buf[:-1].view(torch.int64)[tok_at:tok_at + n]
+                tok.copy_(tokens_of("skewed", n, rows))
+                grad = torch.as_strided(buf, (n, width), (stride, 1), at)
+                acc = buf[acc_at:acc_at + size].view(rows, width)
+                read = set(range(2 * tok_at, 2 * tok_at + 2 * n))
+                for i in range(n):
+                    read.update(range(at + i * stride, at + i * stride + width))
+                before = buf.clone()
+                if read.isdisjoint(range(acc_at, acc_at + size)):
+                    check(acc, tok, grad, 0.5)
+                    added += 1
+                else:
+                    with pytest.raises(B.SoloError) as e:
+                        B.solo_grad_accumulate_rows(acc, tok, grad, scale=0.5)
+                    assert e.value.status == B.SOLO_EINVAL
+                    assert torch.equal(buf.view(torch.int32), before.view(torch.int32))
+                    refused += 1
+    assert refused > 20 and added > 20
+    acc = torch.zeros(5, 8, device="cuda")
+    with pytest.raises(B.SoloError):
+        B.solo_grad_accumulate_rows(acc, acc.view(torch.int64).view(-1)[:3], torch.ones(3, 8, device="cuda"))
+    assert float(acc.abs().sum()) == 0.0

@@ -76,3 +76,34 @@ def test_rows_are_checked(B):
         assert call(**kw) == B.SOLO_EALIGN, kw
     assert call(num_tokens=0, tokens=None, grad=None, ws=None) == B.SOLO_OK
     assert L.solo_grad_accumulate_rows(None, 1.0, 256, None) == B.SOLO_EINVAL
+
+
+def test_rows_that_would_be_read_and_written_at_once_are_refused(B):
+    """The accumulator and the workspace against each other, the tokens and the gradient's rows (of numbers, not of memory)."""
+    n, width, rows = 2000, 8, 50                                # not the one-launch form: with a workspace
+    size = C.c_size_t()
+    assert B.lib().solo_grad_rows_workspace(n, width, C.byref(size)) == B.SOLO_OK and size.value
+    at = dict(acc=1 << 20, tokens=2 << 20, grad=3 << 20, ws=4 << 20)
+    bytes_of = dict(acc=rows * width * 4, tokens=n * 8, grad=((n - 1) * width + width) * 4, ws=size.value)
+
+    def call(stride=width, n=n, **kw):
+        p = {**at, **kw}
+        return B.lib().solo_grad_accumulate_rows(C.byref(B.GradRows(p["acc"], rows, width, p["tokens"], 8, 0, p["grad"], stride, n)), 1.0, p["ws"], None)
+
+    for a, b in (("acc", "tokens"), ("acc", "grad"), ("acc", "ws"), ("ws", "tokens"), ("ws", "grad")):
+        for x, y in ((a, b), (b, a)):                           # x begins where y does, ends in it, or begins in its last bytes
+            for place in (at[y], at[y] - bytes_of[x] // 16 * 16 + 16, at[y] + (bytes_of[y] - 1) // 16 * 16):
+                assert call(**{x: place}) == B.SOLO_EINVAL, (x, y, place - at[y])
+    gap = 64 * width                                            # acc within a gap, but for its first or its last bytes
+    assert call(stride=gap, acc=at["grad"] + 5 * gap + width * 4 - 16) == B.SOLO_EINVAL
+    assert call(stride=gap, acc=at["grad"] + 6 * gap * 4 - bytes_of["acc"] + 16) == B.SOLO_EINVAL
+    assert call(stride=0, acc=at["grad"] + width * 4 - 16) == B.SOLO_EINVAL
+    for stride, n_ in ((1 << 60, 3000), ((1 << 60) + 1, 2000), ((1 << 63) - 1, 2), ((1 << 62), 1 << 40)):
+        assert call(stride=stride, n=n_) == B.SOLO_EINVAL, (stride, n_)
+
+
+def test_few_rows_that_would_be_read_and_written_at_once_are_refused(B):
+    rows = lambda acc, tokens, grad, n=3: B.lib().solo_grad_accumulate_rows(  # noqa: E731
+        C.byref(B.GradRows(acc, 5, 8, tokens, 8, 1, grad, 8, n)), 1.0, None, None)
+    for acc, tokens, grad in ((1024, 1024, 4096), (1024, 4096, 1024), (1024, 1024 + 152, 4096), (1024, 1024 - 16, 4096), (1024, 4096, 1024 + 158)):
+        assert rows(acc, tokens, grad) == B.SOLO_EINVAL, (acc, tokens, grad)
