@@ -451,7 +451,7 @@ int solo_grad_norm(const solo_grad_list_t* list, int norm_type, float scale, flo
  * norms of the scaled gradients, as solo_grad_norm gives them.  num_norms = 0: f = scale, a plain
  * scaling or conversion.  `dst` may be `src` (in place; if f is 1 nothing is written then and next to nothing read) or
  * a list of the same sizes and any type.  A norm that is NaN makes everything NaN, an infinite one
- * finite gradients 0; max_norm is finite and not negative.  No tensor of `dst` overlaps another one.
+ * finite gradients 0; max_norm is finite and not negative.  No tensor of `dst` overlaps another one, or `norms_dev`.
  */
 int solo_grad_clip(const solo_grad_list_t* src, const solo_grad_list_t* dst, const float* norms_dev,
                    int num_norms, int norm_type, float max_norm, float scale, void* stream);

@@ -6,6 +6,7 @@ there, loading raises: there is no other implementation to fall back to.
 """
 from __future__ import annotations
 
+import bisect
 import ctypes as C
 import functools
 import math
@@ -457,7 +458,8 @@ class GradSet:
         _check(lib().solo_grads_create(arr, len(grads), self.geom.data_ptr(), _stream(), C.byref(self.handle)), "solo_grads_create")
         # a list that is written must not have two tensors over the same memory
         self._spans = [(p, p + n * grads[0].element_size()) for p, n in zip(ptrs, self.sizes) if n]
-        self._apart = _disjoint(sorted(self._spans))
+        self._in_order = sorted(self._spans)
+        self._apart = _disjoint(self._in_order)
         self._low, self._high = min((a for a, _ in self._spans), default=0), max((b for _, b in self._spans), default=0)
         self._clear_of = {}           # lists that this one was found to lie clear of, by id
         n = C.c_size_t()
@@ -516,6 +518,12 @@ def _written(gs: GradSet, read: GradSet):
     return gs._ref
 
 
+def _reaches_into(low: int, high: int, apart: list) -> bool:
+    """Whether [low, high) shares memory with one of the spans, which are in order and apart."""
+    i = bisect.bisect_left(apart, (high,))
+    return i > 0 and apart[i - 1][1] > low
+
+
 def _norm_type(p) -> int:
     if p not in _NORM_TYPE:
         raise ValueError("norm_type must be 1, 2 or infinity")
@@ -537,15 +545,18 @@ def solo_grad_norm(gs: GradSet, norm_type=2, scale: float = 1.0, per_tensor: boo
 
 def solo_grad_clip(src: GradSet, norms, max_norm: float, dst: GradSet = None, norm_type=2, scale: float = 1.0) -> None:
     """dst (default: src, in place) = src * scale * min(1, max_norm / (N + 1e-6)), N the norm of the whole from the
-    `norms` of its parts (a float32 CUDA tensor); norms=None: scaling and conversion alone."""
-    n = 0
+    `norms` of its parts (a float32 CUDA tensor, outside of dst); norms=None: scaling and conversion alone."""
+    n, to = 0, dst or src
     if norms is not None:
         if not isinstance(norms, torch.Tensor) or not norms.is_cuda or norms.dtype != torch.float32 or not norms.is_contiguous() or norms.device != src.device:
             raise ValueError("norms must be a contiguous float32 tensor on the gradients' device")
         n = norms.numel()
         if n == 0:
             raise ValueError("norms has no element")
-    rc = (_lib or lib()).solo_grad_clip(src._ref, _written(dst or src, src), norms.data_ptr() if n else None, n,
+        at = norms.data_ptr()
+        if at < to._high and to._low < at + 4 * n and to._apart and _reaches_into(at, at + 4 * n, to._in_order):
+            raise ValueError("norms must not lie in what is written")
+    rc = (_lib or lib()).solo_grad_clip(src._ref, _written(to, src), at if n else None, n,
                                         _norm_type(norm_type), max_norm if n else 0.0, scale, _stream())
     if rc:
         _check(rc, "solo_grad_clip")

@@ -473,3 +473,26 @@ def test_refusals():
     wrong = B.GradList(a.handle.value, a.ptrs.data_ptr(), 3)
     assert L.solo_grad_norm(B.C.byref(wrong), 2, 1.0, out.data_ptr(), None, ws.data_ptr(), None) == B.SOLO_EINVAL
     assert float(x.sum()) == 100.0
+
+
+def test_norms_in_what_a_clip_writes():
+    """Every CTA reads the norms for itself while others write: refused where they lie in dst, not beside or in what is only read."""
+    B = lib()
+    z = torch.ones(1000, device="cuda")
+    far = torch.zeros(400, device="cuda")
+    gs = B.GradSet([z[:100], z[200:300], z[400:400], z[500:700]])
+    out = B.GradSet([far[:100], far[100:200], far[0:0], far[200:400]])
+    for norms in (z[0:1], z[99:101], z[98:202], z[200:201], z[299:300], z[499:501], z[699:702], z[:900]):
+        with pytest.raises(ValueError):
+            B.solo_grad_clip(gs, norms, 0.5)
+    assert bool((z == 1).all())
+    B.solo_grad_clip(gs, z[99:101], 1.0, dst=out)                               # in the source, which is read alone
+    near(far, torch.full_like(far, 1.0).double() / (math.sqrt(2.0) + 1e-6), 3 * U)
+    beside = (z[100:101], z[300:400], z[400:401], z[499:500], z[700:702], z[999:])
+    for k, norms in enumerate(beside):
+        norms.fill_(1.0)
+        want = z[0].double() * (0.5 / (math.sqrt(norms.numel()) + 1e-6))
+        B.solo_grad_clip(gs, norms, 0.5)
+        for part in (z[:100], z[200:300], z[500:700]):
+            near(part, want.expand(part.shape), 4 * U * (k + 1))
+        assert bool((norms == 1).all())

@@ -107,3 +107,12 @@ def test_few_rows_that_would_be_read_and_written_at_once_are_refused(B):
         C.byref(B.GradRows(acc, 5, 8, tokens, 8, 1, grad, 8, n)), 1.0, None, None)
     for acc, tokens, grad in ((1024, 1024, 4096), (1024, 4096, 1024), (1024, 1024 + 152, 4096), (1024, 1024 - 16, 4096), (1024, 4096, 1024 + 158)):
         assert rows(acc, tokens, grad) == B.SOLO_EINVAL, (acc, tokens, grad)
+
+
+def test_spans_that_share_memory(B):
+    spans = [(10, 20), (20, 25), (40, 41), (60, 100)]
+    taken = {x for a, b in spans for x in range(a, b)}
+    for low in range(0, 110):
+        for length in (1, 2, 4, 15, 40, 120):
+            assert B._reaches_into(low, low + length, spans) == (not taken.isdisjoint(range(low, low + length))), (low, length)
+    assert not B._reaches_into(0, 1 << 60, [])
