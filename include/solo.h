@@ -426,9 +426,9 @@ int solo_grads_destroy(solo_grads_t* grads);
 int solo_grads_workspace(const solo_grads_t* grads, size_t* bytes);
 
 /*
- * A list of gradient tensors.  The struct is host memory; `data` is a DEVICE array with a device
- * pointer for each tensor (aligned to its elements; 16-byte aligned tensors run faster), which a
- * call reads when it runs.  Tensors of two lists of a call do not overlap, but for the same list given twice.
+ * A list of gradient tensors.  The struct is host memory; `data` is a DEVICE array (8-byte aligned, as floats are 4-byte
+ * aligned: SOLO_EALIGN) with a device pointer for each tensor, aligned to its elements (not checked; 16-byte aligned tensors
+ * run faster), which a call reads when it runs.  Tensors of two lists of a call do not overlap, but for the same list given twice.
  */
 typedef struct {
     const solo_grads_t* grads;

@@ -10,6 +10,7 @@ import bisect
 import ctypes as C
 import functools
 import math
+import operator
 import threading
 import weakref
 from pathlib import Path
@@ -451,6 +452,7 @@ class GradSet:
         self.grads, self.dtype, self.device = list(grads), dtype, dev
         self.sizes = [g.numel() for g in grads]
         ptrs = [g.data_ptr() for g in grads]
+        _aligned(ptrs, grads[0].element_size())
         self.ptrs = torch.tensor(ptrs, dtype=torch.int64).to(dev, non_blocking=True)      # staged before it returns
         self.geom = torch.empty(2 * len(grads) + 1, dtype=torch.int64, device=dev)
         self.handle = C.c_void_p()
@@ -488,6 +490,11 @@ class GradSet:
 
     def _norms(self, per_tensor: bool) -> torch.Tensor:
         return torch.empty(1 + len(self.sizes) if per_tensor else 1, dtype=torch.float32, device=self.device)
+
+
+def _aligned(ptrs: list, size: int) -> None:
+    if functools.reduce(operator.or_, ptrs) & (size - 1):         # (memory of other libraries may begin anywhere)
+        raise ValueError("gradients must be aligned to their elements")
 
 
 def _disjoint(spans) -> bool:

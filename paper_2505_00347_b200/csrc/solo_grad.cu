@@ -593,6 +593,7 @@ bool valid_norm(int n) { return n >= SOLO_NORM_MAX && n <= SOLO_NORM_2; }
 
 int check_list(const solo_grad_list_t* l) {
     if (!l || !l->grads || !l->data || !valid_dtype(l->dtype)) return SOLO_EINVAL;
+    if ((uintptr_t)l->data & 7u) return SOLO_EALIGN;
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return SOLO_ECUDA; }
     return dev == l->grads->device ? SOLO_OK : SOLO_ESTATE;
@@ -605,9 +606,9 @@ int check_pair(const solo_grad_list_t* a, const solo_grad_list_t* b) {
     return a->grads == b->grads || a->grads->numel == b->grads->numel ? SOLO_OK : SOLO_ESTATE;
 }
 
-int check_norm(int norm_type, const float* norm_dev, const void* workspace) {
+int check_norm(int norm_type, const float* norm_dev, const float* tensor_norm_dev, const void* workspace) {
     if (!valid_norm(norm_type) || !norm_dev || !workspace) return SOLO_EINVAL;
-    return ((uintptr_t)workspace & 15u) ? SOLO_EALIGN : SOLO_OK;
+    return (((uintptr_t)norm_dev | (uintptr_t)tensor_norm_dev) & 3u) || ((uintptr_t)workspace & 15u) ? SOLO_EALIGN : SOLO_OK;
 }
 
 // One pass over the list; *grid_out: CTAs launched (what the partials are of).
@@ -740,8 +741,8 @@ int solo_grads_workspace(const solo_grads_t* g, size_t* bytes) {
 
 int solo_grad_norm(const solo_grad_list_t* list, int norm_type, float scale, float* norm_dev, float* tensor_norm_dev,
                    void* workspace_dev, void* stream) {
-    int rc = check_list(list);
-    if (rc == SOLO_OK) rc = check_norm(norm_type, norm_dev, workspace_dev);
+    int rc = check_norm(norm_type, norm_dev, tensor_norm_dev, workspace_dev);
+    if (rc == SOLO_OK) rc = check_list(list);
     if (rc != SOLO_OK) return rc;
     if (!std::isfinite(scale)) return SOLO_EINVAL;
     const GradArgs a = norm_args(list->grads, workspace_dev, scale, norm_dev, tensor_norm_dev, (cudaStream_t)stream);
@@ -753,10 +754,11 @@ int solo_grad_norm(const solo_grad_list_t* list, int norm_type, float scale, flo
 
 int solo_grad_clip(const solo_grad_list_t* src, const solo_grad_list_t* dst, const float* norms_dev, int num_norms, int norm_type,
                    float max_norm, float scale, void* stream) {
-    const int rc = check_pair(src, dst);
-    if (rc != SOLO_OK) return rc;
     if (num_norms < 0 || (num_norms && !norms_dev) || !valid_norm(norm_type)) return SOLO_EINVAL;
     if (!std::isfinite(scale) || (num_norms && !(std::isfinite(max_norm) && max_norm >= 0.0f))) return SOLO_EINVAL;
+    if (num_norms && ((uintptr_t)norms_dev & 3u)) return SOLO_EALIGN;
+    const int rc = check_pair(src, dst);
+    if (rc != SOLO_OK) return rc;
     GradArgs a;
     std::memset(&a, 0, sizeof(a));
     a.norms = norms_dev;
@@ -769,8 +771,8 @@ int solo_grad_clip(const solo_grad_list_t* src, const solo_grad_list_t* dst, con
 
 int solo_grad_clip_norm(const solo_grad_list_t* src, const solo_grad_list_t* dst, int norm_type, float max_norm, float scale,
                         float* norm_dev, float* tensor_norm_dev, void* workspace_dev, void* stream) {
-    int rc = check_pair(src, dst);
-    if (rc == SOLO_OK) rc = check_norm(norm_type, norm_dev, workspace_dev);
+    int rc = check_norm(norm_type, norm_dev, tensor_norm_dev, workspace_dev);
+    if (rc == SOLO_OK) rc = check_pair(src, dst);
     if (rc != SOLO_OK) return rc;
     if (!std::isfinite(scale) || !std::isfinite(max_norm) || !(max_norm >= 0.0f)) return SOLO_EINVAL;
     // the clip finishes the total itself, from the sums, and so needs the workspace for itself until it has run
@@ -797,16 +799,13 @@ int solo_grad_clip_norm(const solo_grad_list_t* src, const solo_grad_list_t* dst
 
 int solo_grad_accumulate(const solo_grad_list_t* acc, const solo_grad_list_t* grad, float scale, int first, int norm_type,
                          float* norm_dev, float* tensor_norm_dev, void* workspace_dev, void* stream) {
-    int rc = check_pair(acc, grad);
+    int rc = norm_type == -1 ? SOLO_OK : check_norm(norm_type, norm_dev, tensor_norm_dev, workspace_dev);
+    if (rc == SOLO_OK) rc = check_pair(acc, grad);
     if (rc != SOLO_OK) return rc;
     if (acc->dtype != SOLO_DT_F32 || !std::isfinite(scale)) return SOLO_EINVAL;
     GradArgs a;
     std::memset(&a, 0, sizeof(a));
-    if (norm_type != -1) {
-        rc = check_norm(norm_type, norm_dev, workspace_dev);
-        if (rc != SOLO_OK) return rc;
-        a = norm_args(acc->grads, workspace_dev, 1.0f, norm_dev, tensor_norm_dev, (cudaStream_t)stream);
-    }
+    if (norm_type != -1) a = norm_args(acc->grads, workspace_dev, 1.0f, norm_dev, tensor_norm_dev, (cudaStream_t)stream);
     a.scale = scale;
     int grid = 0;
     rc = pass(first ? OP_ACC_FIRST : OP_ACC, grad, acc, norm_type, a, (cudaStream_t)stream, &grid);

@@ -116,3 +116,28 @@ def test_spans_that_share_memory(B):
         for length in (1, 2, 4, 15, 40, 120):
             assert B._reaches_into(low, low + length, spans) == (not taken.isdisjoint(range(low, low + length))), (low, length)
     assert not B._reaches_into(0, 1 << 60, [])
+
+
+def test_pointers_off_their_alignment_are_refused(B):
+    """A list whose sizes are never looked at: pointers are refused before."""
+    L = B.lib()
+    p = lambda data=64: C.byref(B.GradList(64, data, 0))  # noqa: E731
+    for off in (1, 2, 3):
+        for per in (None, 64):
+            assert L.solo_grad_norm(p(), 2, 1.0, 64 + off, per, 64, None) == B.SOLO_EALIGN
+            assert L.solo_grad_clip_norm(p(), p(), 2, 1.0, 1.0, 64 + off, per, 64, None) == B.SOLO_EALIGN
+            assert L.solo_grad_accumulate(p(), p(), 1.0, 0, 2, 64 + off, per, 64, None) == B.SOLO_EALIGN
+        assert L.solo_grad_norm(p(), 2, 1.0, 64, 64 + off, 64, None) == B.SOLO_EALIGN
+        assert L.solo_grad_clip_norm(p(), p(), 2, 1.0, 1.0, 64, 64 + off, 64, None) == B.SOLO_EALIGN
+        assert L.solo_grad_accumulate(p(), p(), 1.0, 1, 1, 64, 64 + off, 64, None) == B.SOLO_EALIGN
+        assert L.solo_grad_clip(p(), p(), 64 + off, 1, 2, 1.0, 1.0, None) == B.SOLO_EALIGN
+    for data in (65, 66, 68, 71):
+        assert L.solo_grad_norm(p(data), 2, 1.0, 64, None, 64, None) == B.SOLO_EALIGN
+        assert L.solo_grad_clip(p(data), p(data), 64, 1, 2, 1.0, 1.0, None) == B.SOLO_EALIGN
+        assert L.solo_grad_clip_norm(p(data), p(data), 2, 1.0, 1.0, 64, None, 64, None) == B.SOLO_EALIGN
+        assert L.solo_grad_accumulate(p(data), p(data), 1.0, 0, -1, None, None, None, None) == B.SOLO_EALIGN
+    for size in (2, 4):
+        B._aligned([0, 64, 64 + size], size)
+        for off in range(1, size):
+            with pytest.raises(ValueError):
+                B._aligned([0, 64 + off, 128], size)
