@@ -17,10 +17,9 @@
 #include <cuda_fp16.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstring>
-#include <map>
-#include <mutex>
 #include <new>
 #include <vector>
 
@@ -537,21 +536,19 @@ GradKernel grad_kernel_for(int op, int ds, int dd, int nt) {
     }
 }
 
-// Resident CTAs per SM, at most GCTAS_PER_SM; 0 on error.
-int grad_occupancy(GradKernel k, int device) {
-    static std::mutex mu;
-    static std::map<std::pair<int, const void*>, int> cache;
-    std::lock_guard<std::mutex> lk(mu);
-    const auto key = std::make_pair(device, (const void*)k);
-    const auto it = cache.find(key);
-    if (it != cache.end()) return it->second;
-    int n = 0;
+// Resident CTAs per SM of grad_kernel_for's kernel, at most GCTAS_PER_SM; 0 on error.  Remembered in place: a map would allocate, and
+// what that throws would leave through the C calls.
+int grad_occupancy(GradKernel k, int op, int ds, int dd, int nt, int device) {
+    static std::atomic<int8_t> seen[64][4][3][3][4];
+    std::atomic<int8_t>* const at = device >= 0 && device < 64 ? &seen[device][op][ds][dd][nt + 1] : nullptr;
+    int n = at ? at->load(std::memory_order_relaxed) : 0;
+    if (n > 0) return n;
     if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, (const void*)k, GCTA, 0) != cudaSuccess) {
         cudaGetLastError();
         return 0;
     }
     n = std::min(n, GCTAS_PER_SM);
-    cache[key] = n;
+    if (at) at->store((int8_t)n, std::memory_order_relaxed);
     return n;
 }
 
@@ -615,9 +612,10 @@ int check_norm(int norm_type, const float* norm_dev, const float* tensor_norm_de
 int pass(int op, const solo_grad_list_t* src, const solo_grad_list_t* dst, int norm_type, GradArgs a, cudaStream_t stream,
          int* grid_out = nullptr) {
     const solo_grads* g = src->grads;
-    const GradKernel k = grad_kernel_for(op, src->dtype, dst ? dst->dtype : 0, norm_type);
+    const int dd = dst ? dst->dtype : 0;
+    const GradKernel k = grad_kernel_for(op, src->dtype, dd, norm_type);
     if (!k) return SOLO_EINVAL;
-    const int per_sm = grad_occupancy(k, g->device);
+    const int per_sm = grad_occupancy(k, op, src->dtype, dd, norm_type, g->device);
     if (per_sm <= 0) return SOLO_ECUDA;
     a.src = (const void* const*)src->data;
     a.dst = dst ? dst->data : nullptr;

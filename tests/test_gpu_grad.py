@@ -496,3 +496,69 @@ def test_norms_in_what_a_clip_writes():
         for part in (z[:100], z[200:300], z[500:700]):
             near(part, want.expand(part.shape), 4 * U * (k + 1))
         assert bool((norms == 1).all())
+
+
+NO_MEMORY = r"""
+#include <cstdlib>
+#include <new>
+static thread_local bool armed;
+extern "C" void no_memory(int on) { armed = on != 0; }
+void* operator new(std::size_t n) {
+    void* const p = armed ? nullptr : std::malloc(n ? n : 1);
+    if (!p) throw std::bad_alloc();
+    return p;
+}
+void* operator new[](std::size_t n) { return operator new(n); }
+void operator delete(void* p) noexcept { std::free(p); }
+void operator delete[](void* p) noexcept { std::free(p); }
+void operator delete(void* p, std::size_t) noexcept { std::free(p); }
+void operator delete[](void* p, std::size_t) noexcept { std::free(p); }
+"""
+
+CALLS_WITHOUT_MEMORY = """
+import ctypes as C, itertools, sys
+sys.path.insert(0, sys.argv[1])
+import torch
+from paper_2505_00347_b200 import binding as B
+no_memory = C.CDLL(sys.argv[2]).no_memory
+types = (torch.float32, torch.bfloat16, torch.float16)
+lists = [B.GradSet([torch.ones(9000, device="cuda", dtype=t), torch.ones(5, device="cuda", dtype=t)]) for t in types]
+acc = B.GradSet([torch.ones(9000, device="cuda"), torch.ones(5, device="cuda")])
+out = B.GradSet([torch.ones(9000, device="cuda"), torch.ones(5, device="cuda")])
+ws = torch.zeros(lists[0]._workspace_bytes, dtype=torch.uint8, device="cuda")
+norm = torch.zeros(1, device="cuda")
+L, at, w, s = B.lib(), norm.data_ptr(), ws.data_ptr(), B._stream()
+sizes, geom, handle = (C.c_int64 * 2)(9000, 5), torch.empty(5, dtype=torch.int64, device="cuda"), C.c_void_p()
+
+def call(status, f, *args):
+    torch.cuda.synchronize()
+    no_memory(1)
+    rc = f(*args)
+    no_memory(0)
+    assert rc == status, (f.__name__, rc)
+
+call(B.SOLO_ENOMEM, L.solo_grads_create, sizes, 2, geom.data_ptr(), s, C.byref(handle))
+assert not handle.value
+for l, p in itertools.product(lists, (0, 1, 2)):
+    call(B.SOLO_OK, L.solo_grad_norm, l._ref, p, 1.0, at, None, w, s)
+    call(B.SOLO_OK, L.solo_grad_clip_norm, l._ref, out._ref, p, 1e9, 1.0, at, None, w, s)
+    call(B.SOLO_OK, L.solo_grad_accumulate, acc._ref, l._ref, 1.0, 1, p, at, None, w, s)
+    call(B.SOLO_OK, L.solo_grad_accumulate, acc._ref, l._ref, 1.0, 0, p, at, None, w, s)
+torch.cuda.synchronize()
+assert abs(float(norm) / (2.0 * 9005 ** 0.5) - 1) < 1e-6, float(norm)
+print("done")
+"""
+
+
+def test_calls_without_host_memory(tmp_path):
+    """Nothing throws: with no memory to be had, a list is refused and the other calls, which allocate nothing, run as ever."""
+    import os
+    import subprocess
+    import sys
+    shim, source = tmp_path / "no_memory.so", tmp_path / "no_memory.cpp"
+    source.write_text(NO_MEMORY)
+    subprocess.run(["g++", "-O1", "-shared", "-fPIC", "-o", str(shim), str(source)], check=True)
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", CALLS_WITHOUT_MEMORY, root, str(shim)], env={**os.environ, "LD_PRELOAD": str(shim)},
+                       capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "done" in r.stdout, (r.returncode, r.stdout[-500:], r.stderr[-2000:])
