@@ -141,3 +141,31 @@ def test_pointers_off_their_alignment_are_refused(B):
         for off in range(1, size):
             with pytest.raises(ValueError):
                 B._aligned([0, 64 + off, 128], size)
+
+
+def test_what_a_list_knows_of_others_goes_with_them(B):
+    """A list of accumulators that sees new gradients in every step, between its own tensors, keeps nothing of the old ones."""
+    import gc
+    import weakref
+
+    def gs(spans, dtype=0):
+        g = object.__new__(B.GradSet)
+        g._spans, g._in_order, g._apart, g.dtype, g._ref = spans, sorted(spans), True, dtype, spans
+        g._low, g._high, g._clear_of = min(a for a, _ in spans), max(b for _, b in spans), weakref.WeakSet()
+        return g
+
+    acc = gs([(0, 10), (1000, 1010)])
+    kept = [gs([(20, 30), (40 + k, 50 + k)]) for k in range(3)]
+    for other in kept * 2:
+        assert B._written(acc, other) is acc._ref
+    assert len(acc._clear_of) == 3
+    for k in range(200):
+        B._written(acc, gs([(100 + k, 105 + k)]))
+        with pytest.raises(ValueError):
+            B._written(acc, gs([(100, 105), (5, 15)]))
+    gc.collect()
+    assert len(acc._clear_of) == 3 and len(list(acc._clear_of)) == 3
+    del kept, other
+    gc.collect()
+    assert len(acc._clear_of) == 0
+    assert B._written(acc, gs([(0, 10), (1000, 1010)])) is acc._ref             # the same tensors: in place
