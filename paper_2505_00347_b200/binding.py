@@ -485,7 +485,11 @@ class GradSet:
             return torch.empty(self._workspace_bytes, dtype=torch.uint8, device=self.device)
         ws = self._workspaces.get(stream)
         if ws is None:
-            ws = self._workspaces.setdefault(stream, torch.zeros(self._workspace_bytes, dtype=torch.uint8, device=self.device))
+            ws = torch.zeros(self._workspace_bytes, dtype=torch.uint8, device=self.device)
+            # kept for a stream of the list's device alone: another device's may have the same handle, and its call is refused; the
+            # zeros would then be of no stream that a later call follows
+            if self.device.index == _current_device():
+                self._workspaces[stream] = ws
         return ws
 
     def _norms(self, per_tensor: bool) -> torch.Tensor:

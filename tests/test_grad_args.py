@@ -169,3 +169,19 @@ def test_what_a_list_knows_of_others_goes_with_them(B):
     gc.collect()
     assert len(acc._clear_of) == 0
     assert B._written(acc, gs([(0, 10), (1000, 1010)])) is acc._ref             # the same tensors: in place
+
+
+def test_workspaces_belong_to_streams_of_the_lists_device(B, monkeypatch):
+    """With another device current the call is refused; what was zeroed for it must not stay under its stream's handle."""
+    import torch
+    g = object.__new__(B.GradSet)
+    g._workspaces, g._workspace_bytes, g.device = {}, 64, torch.device("cuda", 0)
+    made = []
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    monkeypatch.setattr(torch, "zeros", lambda n, dtype, device: made.append(device) or object())
+    monkeypatch.setattr(B, "_current_device", lambda: 1)
+    g._workspace(0)
+    assert g._workspaces == {}
+    monkeypatch.setattr(B, "_current_device", lambda: 0)
+    ws = g._workspace(0)
+    assert g._workspace(0) is ws and g._workspace(7) is not ws and len(g._workspaces) == 2 and len(made) == 3
