@@ -562,3 +562,64 @@ def test_calls_without_host_memory(tmp_path):
     r = subprocess.run([sys.executable, "-c", CALLS_WITHOUT_MEMORY, root, str(shim)], env={**os.environ, "LD_PRELOAD": str(shim)},
                        capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and "done" in r.stdout, (r.returncode, r.stdout[-500:], r.stderr[-2000:])
+
+
+def whole_numbers(n, seed, most=128):
+    """Whole multiples of 2^-14 up to most 2^-14: bf16 holds them, and binary32 every sum of a few of them, so nothing is rounded."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return (torch.randint(-most, most + 1, (n,), generator=g, device="cuda").float() * 2.0 ** -14).bfloat16()
+
+
+def step_on(B, sizes, params, grads):
+    """The optimizer's first step; parameters and state after it."""
+    params, state = [p.clone() for p in params], B.State(list(sizes), 3, 3)
+    B.solo_multi_step(B.TensorSet(params, grads, state), B.hyper(lr=1e-3, beta1=0.6, weight_decay=0.01, seed=5), 1)
+    return params, [state.raw_get(k) for k in ("codes_m", "codes_v", "scale_m", "scale_v", "alpha")]
+
+
+def same_step(a, b):
+    for x, y in zip((*a[0], *a[1]), (*b[0], *b[1])):
+        assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+
+
+@pytest.mark.parametrize("own_norm", [False, True])
+def test_step_on_clipped_accumulators_and_on_gradients_made_in_torch(own_norm):
+    """Accumulators of whole numbers hold exact sums; from the norm that the call returns, the clip is a factor in binary64, rounded
+    to binary32, a product in binary32 and a rounding to bf16.  Torch makes the same gradients, bit for bit, and the same step."""
+    B = lib()
+    sizes = (2048 * 9 + 700, 643, 2048 * 4, 77)
+    w = synth.workload(2, sizes=sizes)
+    params = [synth.make_param(w, i).cuda() for i in range(len(sizes))]
+    micro = [[whole_numbers(n, 10 * t + i) for i, n in enumerate(sizes)] for t in range(4)]
+    acc = [torch.full((n,), math.nan, device="cuda") for n in sizes]
+    grads = [torch.zeros(n, device="cuda", dtype=torch.bfloat16) for n in sizes]
+    al, gl = B.GradSet(acc), B.GradSet(grads)
+    for t, g in enumerate(micro):
+        norm = B.solo_grad_accumulate(al, B.GradSet(g), scale=0.25, first=t == 0, norm_type=2 if t == 3 else None)
+    sums = [sum(m[i].double() for m in micro) * 0.25 for i in range(len(sizes))]
+    for a, x in zip(acc, sums):
+        assert torch.equal(a.double(), x)
+    N = math.sqrt(sum(float(x.square().sum()) for x in sums))
+    near_number(norm, N, NORM_TOL[2])
+    limit = float(torch.tensor(0.3 * N))
+    if own_norm:
+        norm = B.solo_grad_clip_norm(al, limit, dst=gl)
+        near_number(norm, N, NORM_TOL[2])
+        return same_step(step_on(B, sizes, params, grads), step_on(B, sizes, params, made_in_torch(sums, grads, limit, N)))
+    B.solo_grad_clip(al, norm, limit, dst=gl)
+    f = torch.tensor(min(1.0, limit / (float(norm) + 1e-6)), dtype=torch.float32, device="cuda")
+    want = [(x.float() * f).bfloat16() for x in sums]
+    for g, x in zip(grads, want):
+        assert torch.equal(g, x) and int(x.count_nonzero()) > 0
+    same_step(step_on(B, sizes, params, grads), step_on(B, sizes, params, want))
+
+
+def made_in_torch(sums, grads, limit, N):
+    """The clip's own norm is in binary64 and rounded for the caller only, so its factor is one of a few next to this one."""
+    f = torch.tensor(limit / (N + 1e-6), dtype=torch.float32, device="cuda")
+    for steps in range(-12, 13):                                        # 10 u of the norm and a rounding: 11 u, 2 u a step
+        at = (f.view(torch.int32) + steps).view(torch.float32)
+        want = [(x.float() * at).bfloat16() for x in sums]
+        if all(torch.equal(g, x) for g, x in zip(grads, want)):
+            return want
+    raise AssertionError("no factor near the formula's gives these gradients")
