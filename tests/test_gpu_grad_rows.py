@@ -264,3 +264,59 @@ def test_accumulators_next_to_and_over_what_is_read():
     with pytest.raises(B.SoloError):
         B.solo_grad_accumulate_rows(acc, acc.view(torch.int64).view(-1)[:3], torch.ones(3, 8, device="cuda"))
     assert float(acc.abs().sum()) == 0.0
+
+
+@pytest.mark.parametrize("n", [200, 1000, 1024, 1025, 4000, 5000, 65536, 140000])
+@pytest.mark.parametrize("period", [1, 16, 17, 24, 33, 64, 96, 200, 1 << 20])
+def test_few_additions_follow_one_another_in_binary32(n, period):
+    """Fewer than 48, and one rounding besides for every 65,536 tokens.  A large row and then small ones, each a little over half
+    of its last place: wherever such a one is added to a sum that begins with the large row, u of that sum is lost, always to the
+    same side.  (Additions: 23 in a warp that takes 16 rows and 8 more, 7 over the warps, 1 to binary32; in the one-launch form 31,
+    3 and 7.)"""
+    B = lib()
+    i = torch.arange(n, device="cuda")
+    column = torch.where(i % period == 0, 1.0, 2.0 ** -24 * (1 + 2.0 ** -10))
+    for width in (8, 5):
+        grad = (column[:, None] * torch.tensor([1.0, 3.0, -1.0, 0.5, 1024.0, 1.0, 1.0, -7.0], device="cuda")[:width]).contiguous()
+        for scale in (1.0, -0.375):
+            acc = torch.zeros(3, width, device="cuda")
+            B.solo_grad_accumulate_rows(acc, torch.ones(n, dtype=torch.int64, device="cuda"), grad, scale=scale)
+            added = grad.double().abs().sum(0) * abs(scale)
+            want = grad.double().sum(0) * scale
+            off = (acc[1].double() - want).abs() - (48 + -(-n // CHUNK)) * U * added
+            assert float(off.max()) <= 0, float(((acc[1].double() - want).abs() / (U * added)).max())
+            assert float(acc[0].abs().sum()) + float(acc[2].abs().sum()) == 0.0
+
+
+@pytest.mark.parametrize("n", [500, 3000, 9000])
+def test_rows_clip_and_step_on_gradients_made_in_torch(n):
+    """Rows of whole numbers into an embedding's accumulator, the clip of the whole list by its norm, the step: the same, bit for bit,
+    as the step on gradients that torch made with the operations of the formulas."""
+    from test_gpu_grad import same_step, step_on, whole_numbers
+    B = lib()
+    rows, width = 300, 40
+    sizes = (rows * width, 5000)
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    tok = tokens_of("skewed", n, rows, seed=n).cuda()
+    tok[::7] = -100
+    out, rest = whole_numbers(n * width, n, most=8).view(n, width), whole_numbers(sizes[1], n + 1)
+    acc = [torch.zeros(rows, width, device="cuda"), torch.empty(sizes[1], device="cuda")]
+    grads = [torch.empty(k, dtype=torch.bfloat16, device="cuda") for k in sizes]
+    params = [torch.randn(k, generator=gen, device="cuda") for k in sizes]
+    B.solo_grad_accumulate_rows(acc[0], tok, out, scale=0.5)
+    B.solo_grad_accumulate(B.GradSet(acc[1:]), B.GradSet([rest]), scale=0.5, first=True)
+    keep = tok >= 0
+    table = torch.zeros(rows, width, dtype=torch.float64, device="cuda").index_add_(0, tok[keep], out[keep].double() * 0.5)
+    assert torch.equal(acc[0].double(), table)                              # below 2^24 multiples of 2^-15: nothing is rounded
+    whole = [table.view(-1), rest.double() * 0.5]
+    al = B.GradSet(acc)
+    norm = B.solo_grad_norm(al)
+    N = math.sqrt(sum(float(x.square().sum()) for x in whole))
+    assert abs(float(norm) / N - 1) <= 10 * U
+    limit = float(torch.tensor(0.2 * N))
+    B.solo_grad_clip(al, norm, limit, dst=B.GradSet(grads))
+    f = torch.tensor(limit / (float(norm) + 1e-6), dtype=torch.float32, device="cuda")
+    want = [(x.float() * f).bfloat16() for x in whole]
+    for g, x in zip(grads, want):
+        assert torch.equal(g, x) and int(x.count_nonzero()) > 0
+    same_step(step_on(B, sizes, params, grads), step_on(B, sizes, params, want))
