@@ -462,8 +462,9 @@ class GradSet:
         self._spans = [(p, p + n * grads[0].element_size()) for p, n in zip(ptrs, self.sizes) if n]
         self._in_order = sorted(self._spans)
         self._apart = _disjoint(self._in_order)
-        self._low, self._high = min((a for a, _ in self._spans), default=0), max((b for _, b in self._spans), default=0)
-        self._clear_of = weakref.WeakSet()           # lists that this one was found to lie clear of
+        self._low = self._in_order[0][0] if self._spans else 0
+        self._high = 0 if not self._spans else self._in_order[-1][1] if self._apart else max(b for _, b in self._spans)
+        self._clear_of = None         # set of the lists that this one was found to lie clear of
         n = C.c_size_t()
         _check(lib().solo_grads_workspace(self.handle, C.byref(n)), "solo_grads_workspace")
         self.desc = GradList(self.handle.value, self.ptrs.data_ptr(), _GRAD_DTYPE[dtype])
@@ -520,10 +521,12 @@ def _written(gs: GradSet, read: GradSet):
     if not gs._apart:
         raise ValueError("tensors of a list that is written must not overlap")
     if read is not gs and read._low < gs._high and gs._low < read._high:
-        if read not in gs._clear_of:
+        if gs._clear_of is None or read not in gs._clear_of:
             same = read._spans == gs._spans and read.dtype == gs.dtype
             if not same and not _disjoint(sorted(gs._spans + _union(read._spans))):
                 raise ValueError("the lists of a call must not overlap, unless they are the same")
+            if gs._clear_of is None:
+                gs._clear_of = weakref.WeakSet()
             gs._clear_of.add(read)
     return gs._ref
 
