@@ -399,10 +399,14 @@ int solo_static_status(int* status_out, void* stream);
  *     solo_grad_norm on each worker's shard, an all-gather of one float, solo_grad_clip
  *   solo_multi_step on the bf16 gradients
  *
- * Sums are taken in binary32 over at most 32 elements of a thread and in binary64 from there on, in
- * an order that depends on the tensors' sizes and alignment, the device and whether every tensor's norm is asked for,
- * and on nothing else: the same call on the same inputs gives the same bits.
+ * Sums are taken in binary32 over at most 32 elements of a thread and in binary64 from there on, in an order that depends on
+ * the call, the element and norm types, the tensors' sizes and alignment, the device and whether every tensor's norm is asked
+ * for, and on nothing else: the same call on the same inputs gives the same bits.  (solo_grad_accumulate's norm and
+ * solo_grad_norm of the accumulators that it leaves add in different orders.)
  * Squares that binary32 cannot hold (overflow, underflow) are summed in binary64.
+ *
+ * A list has one element type.  Gradients of several types make a list each: their norms, taken with the same scale, are norms
+ * of parts for solo_grad_clip.
  */
 enum { SOLO_DT_F32 = 0, SOLO_DT_BF16 = 1, SOLO_DT_F16 = 2 };       /* element types of a gradient list */
 enum { SOLO_NORM_MAX = 0, SOLO_NORM_1 = 1, SOLO_NORM_2 = 2 };      /* max |g|, sum |g|, sqrt(sum g^2) */
@@ -415,7 +419,8 @@ typedef struct solo_grads solo_grads_t;
  * `numel_host` is a HOST array; 0 is allowed (an empty tensor), and so are lists with no element at all.
  * `geom_dev` is device memory of 2 * num_tensors + 1 int64 that the caller keeps as long as the handle: the call fills it
  * on `stream` (the values are staged before it returns), and work on other streams has to be ordered after that.  Not while
- * `stream` is capturing (SOLO_EINVAL).  None of the calls on gradients allocates device memory or waits for the device.
+ * `stream` is capturing (SOLO_EINVAL).  This call copies from host memory that is not page-locked, for which CUDA may wait for
+ * `stream`; the others do not wait.  None of the calls on gradients allocates device memory.
  */
 int solo_grads_create(const int64_t* numel_host, int num_tensors, int64_t* geom_dev, void* stream, solo_grads_t** out);
 /* Frees the handle's host memory.  NULL is accepted. */
@@ -429,6 +434,7 @@ int solo_grads_workspace(const solo_grads_t* grads, size_t* bytes);
  * A list of gradient tensors.  The struct is host memory; `data` is a DEVICE array (8-byte aligned, as floats are 4-byte
  * aligned: SOLO_EALIGN) with a device pointer for each tensor, aligned to its elements (not checked; 16-byte aligned tensors
  * run faster), which a call reads when it runs.  Tensors of two lists of a call do not overlap, but for the same list given twice.
+ * norm_dev, tensor_norm_dev and the workspace lie outside of the lists and of each other.
  */
 typedef struct {
     const solo_grads_t* grads;
@@ -445,7 +451,8 @@ int solo_grad_norm(const solo_grad_list_t* list, int norm_type, float scale, flo
                    float* tensor_norm_dev, void* workspace_dev, void* stream);
 
 /*
- * dst = round(src * f), f = scale * min(1, max_norm / (N + 1e-6)), rounded to nearest even.  N is put
+ * dst = round(src * f), f = scale * min(1, max_norm / (N + 1e-6)).  f is computed in binary64 and rounded to binary32 (below
+ * 2^-126 with fewer digits), the product is rounded to binary32 and from there to dst's type, each to nearest even.  N is put
  * together from `norms_dev`, a device array of `num_norms` floats, as the norm of the whole of which
  * these are the norms of the parts (the workers' shards; one value where there are none); they are
  * norms of the scaled gradients, as solo_grad_norm gives them.  num_norms = 0: f = scale, a plain
@@ -475,7 +482,7 @@ int solo_grad_accumulate(const solo_grad_list_t* acc, const solo_grad_list_t* gr
  * The gradient of an embedding, added to its accumulator: acc[tokens[i], :] += scale * grad[i, :], i = 0 .. num_tokens - 1.
  * Tokens outside [0, num_rows) (padding, masked positions) contribute nothing, whatever their rows hold; rows of acc that no
  * token names stay as they are.  The rows of one token are summed in binary32 in groups (fewer than 48 additions follow one another) and
- * the groups in binary64, for 65,536 tokens together; each such sum is added with one rounding.  The order depends on the
+ * the groups in binary64, for 65,536 tokens together; each such sum is rounded to binary32, and added with one more rounding.  The order depends on the
  * tokens and their number, and on the width: the same inputs give the same bits.
  */
 typedef struct {

@@ -433,9 +433,11 @@ _NORM_TYPE = {math.inf: 0, 1: 1, 2: 2}
 
 
 class GradSet:
-    """Descriptor of a list of gradient tensors of one type: fp32, bf16 or fp16 (built once, reused every step).  Made on the
-    current stream; work on other streams is ordered after that by the caller.  It outlives the work and the captured graphs
-    that use it, as the tensors do."""
+    """Descriptor of a list of contiguous gradient tensors of one type: fp32, bf16 or fp16.  Built once and reused every step where
+    the tensors keep their memory, as accumulators do (making one takes the host 20 us and 0.7 us for each tensor); gradients of
+    several types make a list each, whose norms solo_grad_clip joins.  Made on the current stream, not while it is capturing;
+    work on other streams is ordered after that by the caller.  It outlives the work and the captured graphs that use it, as the
+    tensors do."""
 
     def __init__(self, grads: list[torch.Tensor]):
         if not grads:

@@ -623,9 +623,10 @@ int pass(int op, const solo_grad_list_t* src, const solo_grad_list_t* dst, int n
     a.tile_start = g->geom + g->num_tensors;
     a.tiles = g->tiles;
     a.num_tensors = g->num_tensors;
-    // Passes that write run best with no more under way than it takes: three CTAs per SM for 16-bit gradients in place (GB/s with two and three,
-    // 5720 and 6280; 5850 with four or more), two for the others (201M bf16 into fp32 6110 with two, 5660 with three or more; accumulation of
-    // 809M bf16 1235 us with two, 1290 with three to six).  A pass that only reads takes all that fit (7B bf16: 1903 us with four, 1813 with five).
+    // Passes that write run best with no more under way than it takes.  GIN_FLIGHT makes that three CTAs per SM from 16-bit to 16-bit types and two
+    // for all else.  GB/s with two and three, 202M elements: bf16 in place 5680 and 6280, into another list 5910 and 5890; bf16 into fp32 6110
+    // and 5660; accumulation of 809M bf16 1235 us with two, 1290 with three to six.  A pass that only reads takes all that fit (7B bf16: 1903 us
+    // with four, 1813 with five).
     int most = per_sm;
     if (op != OP_NORM) {
         const int written = dst->dtype == SOLO_DT_F32 ? 4 : 2, read = (src->dtype == SOLO_DT_F32 ? 4 : 2) + (op == OP_ACC ? 4 : 0);

@@ -478,7 +478,8 @@ template <int DT, bool VEC, int RV> __global__ __launch_bounds__(ROWS_CTA, SUM_C
     float sum[RV] = {};
     // Entries whose loads are under way together, few enough for four CTAs per SM (eight columns per lane, 16,384 tokens of 4096
     // columns: 2 in four CTAs 67.1 us, 2 in three 72.1, 4 in three 74.5, 2 in five 79), or three with four columns per lane (768 columns 22.6 us,
-    // in four CTAs 23.7) and without wide accesses (4098 columns 91 us, in four CTAs 102, in two 109).
+    // in four CTAs 23.7) and without wide accesses (4098 columns 91 us, in four CTAs 102, in two 109).  (Of calls on the same inputs one after
+    // another; on inputs that change, 768 columns 23.6 us.)
     constexpr int BATCH = RV == WIDE ? 2 : 4;
     constexpr int ES = DT == SOLO_DT_F32 ? 4 : 2;
     if (lane < count) s.entry[warp][lane] = {(const char*)a.grad + pos * a.grad_stride * ES, a.acc + (int64_t)tok * a.width};
@@ -632,7 +633,8 @@ template <int DT, bool VEC> __global__ __launch_bounds__(ROWS_CTA, 4) void rows_
     float old[RV] = {};
     if (alone) cols.load_f32(row, old);
     float total[RV] = {};
-    // (with registers for four CTAs per SM: 1000 tokens of 770 columns 10.0 us, with four rows and what they take 14.3)
+    // (with registers for four CTAs per SM: 1000 tokens of 770 columns 10.0 us, with four rows and what they take 14.3; wide accesses to fp32
+    // spill 24 bytes under that limit)
     constexpr int BATCH = VEC ? 4 : 2;
 #pragma unroll
     for (int k = 0; k < DIRECT_WORDS; ++k) {
